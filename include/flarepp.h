@@ -403,6 +403,120 @@ FLAREPP_API int flarepp_mixer_stage(int stage, int dtype, int64_t B, int64_t N, 
                                     const void* Wo, const void* seeds, void* O, void* ws,
                                     size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Linear layer with its epilogue: the products around the mixer (input and
+ * output projections, the feed-forward half of a block).
+ *   P = X W + bias;  out = residual + act(P)
+ * X [T][K], W [K][N] (out = X W as everywhere), bias [N], residual, out and
+ * pre [T][N], all in dtype; bias, residual and pre may be NULL.  `pre`
+ * receives P rounded to dtype, for the backward; act is applied to P before
+ * that rounding.  Sums, activation and residual are fp32; one rounding at the
+ * end.  Activations: RELU max(P, 0); GELU P Phi(P) with the normal
+ * distribution's Phi; SILU P / (1 + exp(-P)).
+ * T <= 2^30, K and N <= 65536 of any parity, T * max(K, N) <= 2^40 (UNSUPPORTED
+ * beyond).  `out` may be `residual` itself; no other output may overlap an
+ * input or another output.  Workspace: flarepp_linear_workspace_bytes(...)
+ * bytes (0 for an invalid shape).
+ * ------------------------------------------------------------------------- */
+#define FLAREPP_ACT_NONE 0
+#define FLAREPP_ACT_RELU 1
+#define FLAREPP_ACT_GELU 2
+#define FLAREPP_ACT_SILU 3
+FLAREPP_API size_t flarepp_linear_workspace_bytes(int dtype, int64_t T, int64_t K, int64_t N);
+FLAREPP_API int flarepp_linear_forward(int dtype, int act, int64_t T, int64_t K, int64_t N, const void* X,
+                                       const void* W, const void* bias, const void* residual, void* out,
+                                       void* pre, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Backward of the linear layer: with dP = dOut * act'(pre),
+ *   dX = dP W^T [T][K] (dtype: the output gradient of the layer before),
+ *   dW = X^T dP [K][N] and dbias = sum_t dP [N] (fp32), overwritten.
+ * The residual's gradient is dOut itself.  dOut [T][N] (dtype); pre [T][N]
+ * (dtype) is what the forward kept, and may be NULL for ACT_NONE, which does
+ * not read it.  act'(0) = 0 for RELU.  dX, dW and dbias may each be NULL (not
+ * wanted; not all three); X is not read without dW, nor W without dX.
+ * With bf16, dX is made of dP rounded to bf16, dW of dP as two bf16 parts (hi
+ * + lo, ~16 bits: the sums over the tokens keep more bits than one part has),
+ * dbias of dP in fp32.  Sums over the tokens have a fixed order.
+ * Sizes and errors as for the forward; no output may overlap an input or
+ * another output.  Workspace: flarepp_linear_backward_workspace_bytes(...)
+ * bytes (0 for an invalid shape).
+ * ------------------------------------------------------------------------- */
+FLAREPP_API size_t flarepp_linear_backward_workspace_bytes(int dtype, int act, int64_t T, int64_t K, int64_t N);
+FLAREPP_API int flarepp_linear_backward(int dtype, int act, int64_t T, int64_t K, int64_t N, const void* X,
+                                        const void* W, const void* pre, const void* dOut, void* dX, float* dW,
+                                        float* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Embedding lookup: out[t] = scale * table[ids[t]], ids [T] (int64), table
+ * [V][C] and out [T][C] in dtype.  A negative id marks padding: its row is
+ * zero.  An id >= V reads nothing: its row is NaN.  T, V <= 2^30, C <= 65536,
+ * max(T, V) * C <= 2^40 (UNSUPPORTED beyond).
+ *
+ * Backward: dTable[v] = scale * sum of dOut[t] over the t with ids[t] == v,
+ * fp32 [V][C], overwritten (rows that no id names are zero); padding and ids
+ * >= V take no gradient.  dOut [T][C] in dtype: FLAREPP_F32 (as the mixer and
+ * block backward leave dX) or FLAREPP_BF16.  The positions are sorted by
+ * symbol, and the sums, fp32, run over ascending positions in an order that
+ * depends on the ids alone.  Workspace:
+ * flarepp_embedding_backward_workspace_bytes(...) bytes (0 for an invalid
+ * shape).  No output may overlap an input.
+ * ------------------------------------------------------------------------- */
+FLAREPP_API int flarepp_embedding_forward(int dtype, int64_t T, int64_t V, int64_t C, const int64_t* ids,
+                                          const void* table, float scale, void* out, void* stream);
+FLAREPP_API size_t flarepp_embedding_backward_workspace_bytes(int64_t T, int64_t V, int64_t C);
+FLAREPP_API int flarepp_embedding_backward(int dtype, int64_t T, int64_t V, int64_t C, const int64_t* ids,
+                                           const void* dOut, float scale, float* dTable, void* ws,
+                                           size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * AdamW step number `step` (1, 2, ..) over `count` tensors at once:
+ *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay)
+ *       - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in fp32, every operation rounded by itself.  p [n] (fp32) is updated; g [n]
+ * (fp32, as every backward of this library leaves its gradients) is read;
+ * p_low [n], when not NULL, receives p rounded to bf16 (the weights of the
+ * next forward).  p_low may be NULL per tensor.
+ *
+ * FLAREPP_STATE_F32: m and v are fp32 [n]; the scales must be NULL.
+ * FLAREPP_STATE_E4M3: m and r = sqrt(v) are held as e4m3 codes [n] times a
+ * fp32 scale per 256 elements (m_scale, v_scale [ceil(n / 256)]); all zero at
+ * the start.  The update uses m and v before they are rounded.  A scale is
+ * 1 / 448 of its block's largest magnitude (a block below 1e-30 is stored as
+ * zeros), and a value is rounded up or down at random with the probability of
+ * the part cut off, except that a positive r is not rounded to zero: rounded
+ * to nearest, r would stop moving long before v reaches the mean of g^2, since
+ * a step moves it by far less than half a code.  The random bits are a hash of
+ * the step and the element's index, so results are reproducible.  A block with
+ * a gradient that is not finite becomes NaN as a whole.
+ *
+ * `schedule`, when not NULL, is FLAREPP_ADAMW_SCHEDULE_BYTES of device memory
+ * that flarepp_adamw_schedule filled on the host: lr and step are then read
+ * from there when the work runs (the arguments are still checked), so that a
+ * captured graph can take a new step with every replay.
+ * Tensors of any n >= 1 up to 2^40.  Buffers that are written may not overlap
+ * any other buffer of the call (INVALID_ARG).  No workspace.
+ * ------------------------------------------------------------------------- */
+#define FLAREPP_STATE_F32 0
+#define FLAREPP_STATE_E4M3 1
+#define FLAREPP_ADAMW_SCHEDULE_BYTES 24
+typedef struct flarepp_adamw_tensor {
+  int64_t n;
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  void* m_scale;
+  void* v_scale;
+  void* p_low;
+  double weight_decay;
+} flarepp_adamw_tensor;
+FLAREPP_API int flarepp_adamw_schedule(double lr, double beta1, double beta2, int64_t step, void* out);
+FLAREPP_API int flarepp_adamw_step(int state, int64_t count, const flarepp_adamw_tensor* tensors, double lr,
+                                   double beta1, double beta2, double eps, int64_t step, const void* schedule,
+                                   void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -75,6 +75,16 @@ int check_positive(int64_t v, const char* name) {
   return FLAREPP_OK;
 }
 
+}  // namespace
+
+// the last-error record, for the entry points of the other files
+namespace flarepp {
+int api_error(int code, const char* text) { return fail(code, "%s", text); }
+int api_ok() { return ok(); }
+}  // namespace flarepp
+
+namespace {
+
 #define TRY(x) do { int _rc = (x); if (_rc != FLAREPP_OK) return _rc; } while (0)
 #define HIPTRY(x) do { hipError_t _e = (x); if (_e != hipSuccess) \
     return fail(FLAREPP_ERR_HIP, "%s: %s", #x, hipGetErrorString(_e)); } while (0)

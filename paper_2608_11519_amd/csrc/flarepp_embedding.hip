@@ -1,0 +1,334 @@
+// Embedding lookup with scaling and its gradient.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "flarepp_device.hpp"
+#include "flarepp_layers.hpp"
+
+namespace flarepp {
+namespace {
+
+int pow2_log2(int64_t n, int most) {  // of the smallest power of two >= n, at most `most`
+  int l = 0;
+  while (l < most && (int64_t(1) << l) < n) ++l;
+  return l;
+}
+
+// N values of T as floats, and back
+template <typename T, int N> constexpr int align_n() { return N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16; }
+template <typename T, int N> __device__ __forceinline__ void load_n(const T* p, float (&v)[N]) {
+  T e[N];
+  __builtin_memcpy(e, __builtin_assume_aligned(p, align_n<T, N>()), N * sizeof(T));
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = to_f32(e[i]);
+}
+template <typename T, int N> __device__ __forceinline__ void store_n(T* p, const float (&v)[N]) {
+  T e[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) e[i] = from_f32<T>(v[i]);
+  __builtin_memcpy(__builtin_assume_aligned(p, align_n<T, N>()), e, N * sizeof(T));
+}
+
+// out[t] = scale * table[ids[t]]: VEC channels per lane, 2^cl lanes across a
+// row, four rows per lane so that their loads are in flight together.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void k_embed(EmbedParams p, int cl) {
+  constexpr int ROWS = 4;
+  const int rl = 256 >> cl, lr = threadIdx.x >> cl;
+  const int64_t col = (((int64_t)blockIdx.y << cl) + (threadIdx.x & ((1 << cl) - 1))) * VEC;
+  const int64_t t0 = (int64_t)blockIdx.x * rl * ROWS + lr;
+  if (col >= p.C) return;
+  int64_t id[ROWS];
+  float v[ROWS][VEC];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) id[r] = t0 + r * rl < p.T ? p.ids[t0 + r * rl] : -1;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (id[r] >= 0 && id[r] < p.V) load_n<T, VEC>(static_cast<const T*>(p.table) + id[r] * p.C + col, v[r]);
+    else
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[r][e] = id[r] < 0 ? 0.f : __builtin_nanf("");
+  }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (t0 + r * rl >= p.T) continue;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[r][e] *= p.scale;
+    store_n<T, VEC>(static_cast<T*>(p.out) + (t0 + r * rl) * p.C + col, v[r]);
+  }
+}
+
+// ---- gradient -------------------------------------------------------------------
+// A stable radix sort of the positions by symbol (ids outside [0, V) sort
+// last, as V), then sums over the runs of equal symbols in ascending position.
+
+__device__ __forceinline__ uint32_t embed_key(const EmbedGradParams& p, int pass, int64_t i) {
+  if (pass > 0) return p.key[pass & 1][i];
+  const int64_t id = p.ids[i];
+  return id < 0 || id >= p.V ? (uint32_t)p.V : (uint32_t)id;
+}
+
+// counts[digit][workgroup]; the first pass also clears the table's gradient
+__global__ __launch_bounds__(256) void k_embed_count(EmbedGradParams p, int pass, int nb) {
+  __shared__ int hist[1024];
+  const int bins = 1 << p.bits, shift = pass * p.bits;
+  for (int b = threadIdx.x; b < bins; b += 256) hist[b] = 0;
+  __syncthreads();
+  const int64_t i0 = (int64_t)blockIdx.x * kEmbedTile;
+#pragma unroll
+  for (int u = 0; u < kEmbedTile / 256; ++u) {
+    const int64_t i = i0 + u * 256 + threadIdx.x;
+    if (i < p.T) atomicAdd(&hist[embed_key(p, pass, i) >> shift & (bins - 1)], 1);
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += 256) p.counts[(int64_t)b * nb + blockIdx.x] = hist[b];
+}
+
+__global__ __launch_bounds__(256) void k_embed_clear(float* p, int64_t n) {
+  const int64_t stride = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n / 4; i += stride)
+    reinterpret_cast<f32x4*>(p)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int64_t tail = n / 4 * 4 + threadIdx.x;
+  if (blockIdx.x == 0 && tail < n) p[tail] = 0.f;
+}
+
+// exclusive sums over the workgroups of a digit, one wave per digit
+__global__ __launch_bounds__(64) void k_embed_scan(EmbedGradParams p, int nb) {
+  int* row = p.counts + (int64_t)blockIdx.x * nb;
+  const int lane = lane_id();
+  int run = 0;
+  for (int b = 0; b < nb; b += 64) {
+    const int v = b + lane < nb ? row[b + lane] : 0;
+    int s = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int o = __shfl_up(s, d);
+      if (lane >= d) s += o;
+    }
+    if (b + lane < nb) row[b + lane] = run + s - v;
+    run += __shfl(s, 63);
+  }
+  if (lane == 0) p.totals[blockIdx.x] = run;
+}
+
+// keys and positions to their places: each wave ranks a run of its
+// workgroup's tile, 64 positions at a time
+__global__ __launch_bounds__(256) void k_embed_scatter(EmbedGradParams p, int pass, int nb) {
+  __shared__ int place[4][1024];
+  __shared__ int sums[256];
+  const int bins = 1 << p.bits, shift = pass * p.bits, lane = lane_id(), wave = wave_id();
+  constexpr int PER = kEmbedTile / 4;  // positions of a wave
+  const int64_t i0 = (int64_t)blockIdx.x * kEmbedTile + wave * PER;
+  uint32_t key[PER / 64];
+#pragma unroll
+  for (int u = 0; u < PER / 64; ++u) {
+    const int64_t i = i0 + u * 64 + lane;
+    key[u] = i < p.T ? embed_key(p, pass, i) : 0;
+  }
+  for (int b = threadIdx.x; b < bins; b += 256)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) place[w][b] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < PER / 64; ++u)
+    if (i0 + u * 64 + lane < p.T) atomicAdd(&place[wave][key[u] >> shift & (bins - 1)], 1);
+  // first place of every digit: sums over the digits (a run of them per thread)
+  const int run = (bins + 255) / 256, b0 = threadIdx.x * run;
+  int total = 0;
+  for (int j = 0; j < run; ++j) total += b0 + j < bins ? p.totals[b0 + j] : 0;
+  sums[threadIdx.x] = total;
+  __syncthreads();
+  for (int d = 1; d < 256; d *= 2) {
+    const int o = threadIdx.x >= (unsigned)d ? sums[threadIdx.x - d] : 0;
+    __syncthreads();
+    sums[threadIdx.x] += o;
+    __syncthreads();
+  }
+  int at = sums[threadIdx.x] - total;
+  for (int j = 0; j < run; ++j) {
+    const int b = b0 + j;
+    if (b >= bins) break;
+    int to = at + p.counts[(int64_t)b * nb + blockIdx.x];
+    at += p.totals[b];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int n = place[w][b];
+      place[w][b] = to;
+      to += n;
+    }
+  }
+  __syncthreads();
+  volatile int* mine = place[wave];  // only this wave reads and writes it from here on
+#pragma unroll
+  for (int u = 0; u < PER / 64; ++u) {
+    const int64_t i = i0 + u * 64 + lane;
+    const bool in = i < p.T;
+    const int digit = (int)(key[u] >> shift & (bins - 1));
+    uint64_t same = __builtin_amdgcn_ballot_w64(in);
+    for (int b = 0; b < p.bits; ++b) {
+      const uint64_t set = __builtin_amdgcn_ballot_w64(digit >> b & 1);
+      same &= digit >> b & 1 ? set : ~set;
+    }
+    if (in) {
+      const int before = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
+      const int first = mine[digit];
+      __builtin_amdgcn_wave_barrier();  // every lane has read the place before its group's last lane moves it
+      const int to = first + before;
+      if ((same >> lane) == 1) mine[digit] = to + 1;
+      p.key[(pass + 1) & 1][to] = key[u];
+      p.pos[(pass + 1) & 1][to] = pass > 0 ? p.pos[pass & 1][i] : (int32_t)i;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Sums over the runs of equal symbols inside chunks of kEmbedChunk sorted
+// positions, 2^cl lanes per chunk and strip of columns.  A run inside one
+// chunk is a row of the result; parts of longer runs go to part[chunk][0]
+// (began before the chunk) or [1] (goes on after it).
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void k_embed_runs(EmbedGradParams p, int cl) {
+  const int64_t col = (((int64_t)blockIdx.y << cl) + (threadIdx.x & ((1 << cl) - 1))) * VEC;
+  const int64_t chunk = ((int64_t)blockIdx.x << (8 - cl)) + (threadIdx.x >> cl);
+  const int64_t i0 = chunk * kEmbedChunk, i1 = min(p.T, i0 + kEmbedChunk);
+  if (i0 >= p.T || col >= p.C) return;
+  const uint32_t* key = p.key[p.passes & 1];
+  const int32_t* pos = p.pos[p.passes & 1];
+  uint32_t cur = key[i0];
+  bool head = i0 > 0 && key[i0 - 1] == cur;
+  float s[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+  auto flush = [&](bool tail) __attribute__((always_inline)) {
+    if (cur >= (uint32_t)p.V) return;  // padding
+    if (head || tail) {
+      store_n<float, VEC>(p.part + (2 * chunk + (head ? 0 : 1)) * p.C + col, s);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[e] *= p.scale;
+      store_n<float, VEC>(p.dtable + (int64_t)cur * p.C + col, s);
+    }
+  };
+  constexpr int AHEAD = 8;
+  for (int64_t i = i0; i < i1; i += AHEAD) {
+    uint32_t k[AHEAD];
+    float v[AHEAD][VEC];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int64_t at = min(i + u, i1 - 1);
+      k[u] = key[at];
+      load_n<T, VEC>(static_cast<const T*>(p.dout) + (int64_t)pos[at] * p.C + col, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if (i + u >= i1) break;
+      if (k[u] != cur) {
+        flush(false);
+        cur = k[u];
+        head = false;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[e] += v[u][e];
+    }
+  }
+  flush(i1 < p.T && key[i1] == cur);
+}
+
+// Rows whose runs cross chunks: the workgroup of the chunk in which a run
+// begins sums its parts, 1024 / 2^cl groups of lanes taking every so many
+// chunks, and then the groups' sums in order.
+template <int VEC>
+__global__ __launch_bounds__(1024) void k_embed_join(EmbedGradParams p, int cl) {
+  __shared__ float sums[1024 * VEC];
+  const int64_t chunk = blockIdx.x, i0 = chunk * kEmbedChunk, i1 = i0 + kEmbedChunk;
+  if (i1 >= p.T) return;
+  const uint32_t* key = p.key[p.passes & 1];
+  const uint32_t cur = key[i1 - 1];
+  if (cur >= (uint32_t)p.V || key[i1] != cur || (i0 > 0 && key[i0 - 1] == cur)) return;  // whole workgroup
+  const int lc = threadIdx.x & ((1 << cl) - 1), lr = threadIdx.x >> cl, rl = 1024 >> cl;
+  const int64_t col = (((int64_t)blockIdx.y << cl) + lc) * VEC;
+  float s[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+  if (col < p.C) {
+    if (lr == 0) load_n<float, VEC>(p.part + (2 * chunk + 1) * p.C + col, s);
+    constexpr int AHEAD = 4;
+    for (int64_t q = chunk + 1 + lr; q * kEmbedChunk < p.T && key[q * kEmbedChunk] == cur; q += AHEAD * rl) {
+      float v[AHEAD][VEC];
+      bool in[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int64_t at = q + u * rl;
+        in[u] = at * kEmbedChunk < p.T && key[at * kEmbedChunk] == cur;
+        if (in[u]) load_n<float, VEC>(p.part + 2 * at * p.C + col, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (in[u])
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) s[e] += v[u][e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sums[threadIdx.x * VEC + e] = s[e];
+  for (int h = rl / 2; h > 0; h /= 2) {
+    __syncthreads();
+    if (lr < h)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sums[threadIdx.x * VEC + e] += sums[(threadIdx.x + (h << cl)) * VEC + e];
+  }
+  if (lr == 0 && col < p.C) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) s[e] = sums[threadIdx.x * VEC + e] * p.scale;
+    store_n<float, VEC>(p.dtable + (int64_t)cur * p.C + col, s);
+  }
+}
+
+template <typename T, int VEC>
+void embed_sums(const EmbedGradParams& p, hipStream_t s) {
+  const int64_t lanes = (p.C + VEC - 1) / VEC, chunks = (p.T + kEmbedChunk - 1) / kEmbedChunk;
+  const int cl = pow2_log2(lanes, 6);
+  const unsigned strips = (unsigned)((lanes + (1 << cl) - 1) >> cl), per = 256u >> cl;
+  k_embed_runs<T, VEC><<<dim3((unsigned)((chunks + per - 1) / per), strips), 256, 0, s>>>(p, cl);
+  if (chunks > 1) k_embed_join<VEC><<<dim3((unsigned)(chunks - 1), strips), 1024, 0, s>>>(p, cl);
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_embed(const EmbedParams& p, hipStream_t s) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool whole = p.C % V == 0;
+  const int64_t lanes = whole ? p.C / V : p.C;
+  const int cl = pow2_log2(lanes, 8), rows = 4 * (256 >> cl);
+  const dim3 grid((unsigned)((p.T + rows - 1) / rows), (unsigned)((lanes + (1 << cl) - 1) >> cl));
+  if (whole) k_embed<T, V><<<grid, 256, 0, s>>>(p, cl);
+  else k_embed<T, 1><<<grid, 256, 0, s>>>(p, cl);
+  return hipGetLastError();
+}
+template hipError_t launch_embed<float>(const EmbedParams&, hipStream_t);
+template hipError_t launch_embed<__bf16>(const EmbedParams&, hipStream_t);
+
+template <typename T>
+hipError_t launch_embed_grad(const EmbedGradParams& p, hipStream_t s) {
+  const int nb = (int)((p.T + kEmbedTile - 1) / kEmbedTile);
+  const int64_t n = p.V * p.C;
+  k_embed_clear<<<dim3((unsigned)std::min<int64_t>(2048, (n + 1023) / 1024)), 256, 0, s>>>(p.dtable, n);
+  for (int pass = 0; pass < p.passes; ++pass) {
+    k_embed_count<<<dim3(nb), 256, 0, s>>>(p, pass, nb);
+    k_embed_scan<<<dim3(1u << p.bits), 64, 0, s>>>(p, nb);
+    k_embed_scatter<<<dim3(nb), 256, 0, s>>>(p, pass, nb);
+  }
+  // 16 bytes of a row of dOut per lane; the sums are stored as whole vectors too
+  constexpr int V = 16 / (int)sizeof(T);
+  if (p.C % V == 0) embed_sums<T, V>(p, s);
+  else embed_sums<T, 1>(p, s);
+  return hipGetLastError();
+}
+template hipError_t launch_embed_grad<float>(const EmbedGradParams&, hipStream_t);
+template hipError_t launch_embed_grad<__bf16>(const EmbedGradParams&, hipStream_t);
+
+}  // namespace flarepp

@@ -1,0 +1,111 @@
+// Parameter blocks and launchers of the operators around the mixer: linear
+// layer, embedding, optimiser step.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace flarepp {
+
+// ---- linear layer ------------------------------------------------------------
+enum Activation { kActNone = 0, kActRelu = 1, kActGelu = 2, kActSilu = 3 };
+
+// The three products of a linear layer, C[P][Q] = sum_k L(p, k) R(k, q), row-major C:
+//   kLinForward  P = tokens, Q = outputs, k = inputs:  L = X rows, R = W
+//   kLinInput    P = tokens, Q = inputs,  k = outputs: L = dP rows, R = W^T
+//   kLinWeight   P = inputs, Q = outputs, k = tokens:  L = X^T, R = dP
+// A k-contiguous operand is stored [rows][K], the others [K][rows] ("T").
+enum LinProduct { kLinForward = 0, kLinInput = 1, kLinWeight = 2 };
+constexpr bool lin_l_t(int prod) { return prod == kLinWeight; }
+constexpr bool lin_r_t(int prod) { return prod != kLinInput; }
+
+// Output tiles (P x Q) of a workgroup
+enum LinTile { kTile128 = 0, kTile64 = 1, kTile128x32 = 2, kTile32x128 = 3 };
+
+struct LinGemmParams {
+  const void* l; const void* r;
+  const void* r_lo;        // kLinWeight, bf16: R = r + r_lo, or null
+  int64_t P, Q, K;
+  int splits; int64_t kchunk;  // split z sums k in [z * kchunk, (z + 1) * kchunk); a multiple of lin_step
+  float* part; int64_t part_stride;  // fp32 sums per split, or null: the epilogue
+  const void* bias; const void* res; void* out; void* pre;
+  int act;
+};
+// reduction elements of one step
+constexpr int lin_step(int elem_bytes) { return 128 / elem_bytes; }
+// Whether the operands can be copied straight to LDS: whole 16-byte chunks,
+// and whole steps where the reduction is contiguous.
+bool lin_direct(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K);
+template <typename T> hipError_t launch_lin_gemm(const LinGemmParams&, int prod, int tile, bool direct, hipStream_t);
+
+// out = epilogue of the sum over the splits of part
+template <typename T> hipError_t launch_lin_finish(const LinGemmParams&, hipStream_t);
+
+// dP = dOut * act'(pre): fp32 type one array, bf16 type hi (+ lo when given);
+// and the column sums of dP per chunk of rows.  act none: sums only.
+struct LinSlopeParams {
+  const void* dout; const void* pre; int act;
+  int64_t T; int64_t N;
+  void* dp; void* dp_lo;   // or null
+  float* part; int64_t part_ld;  // [nchunks][part_ld] column sums, or null
+  int nchunks; int64_t chunk;
+};
+template <typename T> hipError_t launch_lin_slope(const LinSlopeParams&, hipStream_t);
+
+// out[i] = sum_s part[s * stride + i], i < n: two independent jobs in a launch
+struct LinSumJob { const float* part; int64_t stride, n; int splits; float* out; };
+struct LinSumParams { LinSumJob job[2]; int njobs; };
+hipError_t launch_lin_sum(const LinSumParams&, hipStream_t);
+
+// ---- embedding -----------------------------------------------------------------
+struct EmbedParams {
+  const int64_t* ids; const void* table; void* out;
+  int64_t T, V, C;
+  float scale;
+};
+template <typename T> hipError_t launch_embed(const EmbedParams&, hipStream_t);
+
+struct EmbedGradParams {
+  const int64_t* ids; const void* dout;
+  int64_t T, V, C;
+  float scale;
+  float* dtable;
+  // sort workspace: keys and positions of a pass and of the next, counts per
+  // (digit, workgroup) and per digit
+  uint32_t* key[2]; int32_t* pos[2];
+  int32_t* counts; int32_t* totals;
+  float* part;  // [chunks][2][C]: the sums of runs that cross a chunk's start, end
+  int passes, bits;
+};
+constexpr int kEmbedTile = 2048;  // positions of a workgroup of the sort
+constexpr int kEmbedChunk = 64;   // sorted positions summed by one group of lanes
+template <typename T> hipError_t launch_embed_grad(const EmbedGradParams&, hipStream_t);
+
+// ---- optimiser ------------------------------------------------------------------
+constexpr int kAdamwBlock = 256;      // elements that share a scale
+constexpr int kAdamwTurns = 2;        // of them per wave
+constexpr int64_t kAdamwUnit = 4 * kAdamwBlock * kAdamwTurns;  // elements of a workgroup
+constexpr int kAdamwPerLaunch = 40;   // tensors of a launch: their table travels as a kernel argument
+struct AdamwSchedule {
+  double lr;
+  float size;     // lr / (1 - b1^t)
+  float root;     // 1 / sqrt(1 - b2^t)
+  uint32_t step;  // t
+  uint32_t pad;
+};
+struct AdamwTensor {
+  float* p; const float* g; void* m; void* v; float* m_scale; float* v_scale; void* p_low;
+  int64_t n;
+  double decay;
+  int first;   // blocks of the tensors before it in this launch
+};
+struct AdamwParams {
+  AdamwTensor t[kAdamwPerLaunch];
+  int count, blocks;
+  float b1, a1, b2, a2, eps;
+  AdamwSchedule now;              // what changes from step to step,
+  const AdamwSchedule* schedule;  // or null: in device memory
+};
+hipError_t launch_adamw(const AdamwParams&, bool q8, hipStream_t);
+
+}  // namespace flarepp

@@ -1,0 +1,544 @@
+// Linear layer out = res + act(X W + b) and its gradients.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "flarepp_device.hpp"
+#include "flarepp_layers.hpp"
+
+namespace flarepp {
+namespace {
+
+// ---- activations ---------------------------------------------------------------
+// Phi(-|y|), the normal distribution's lower tail, by Abramowitz and Stegun
+// 7.1.26: 1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), absolute
+// error 1.5e-7 in erf.  The tail form keeps it free of cancellation for negative y.
+__device__ __forceinline__ float normal_tail(float y, float& gauss) {
+  const float x = __builtin_fabsf(y) * 0.70710678f;
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
+  gauss = __builtin_amdgcn_exp2f(y * y * -0.72134752f);  // exp(-y^2 / 2)
+  float q = 1.061405429f;
+  q = __builtin_fmaf(q, t, -1.453152027f);
+  q = __builtin_fmaf(q, t, 1.421413741f);
+  q = __builtin_fmaf(q, t, -0.284496736f);
+  q = __builtin_fmaf(q, t, 0.254829592f);
+  return 0.5f * q * t * gauss;
+}
+__device__ __forceinline__ float sigmoid(float y) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y * -1.44269504f));
+}
+__device__ __forceinline__ float activate(float y, int act) {
+  if (act == kActRelu) return y < 0.f ? 0.f : y;  // a NaN stays
+  if (act == kActGelu) {
+    float gauss;
+    const float tail = normal_tail(y, gauss);
+    return y * (y < 0.f ? tail : 1.f - tail);
+  }
+  if (act == kActSilu) return y * sigmoid(y);
+  return y;
+}
+__device__ __forceinline__ float slope(float y, int act) {
+  if (act == kActRelu) return y > 0.f ? 1.f : 0.f;
+  if (act == kActGelu) {
+    float gauss;
+    const float tail = normal_tail(y, gauss);
+    return __builtin_fmaf(y * 0.39894228f, gauss, y < 0.f ? tail : 1.f - tail);
+  }
+  if (act == kActSilu) {
+    const float s = sigmoid(y);
+    return s * __builtin_fmaf(y, 1.f - s, 1.f);
+  }
+  return 1.f;
+}
+
+// ---- operand tiles in LDS ----------------------------------------------------------
+// A step holds 128 bytes of the reduction of every row.  k-contiguous operands
+// lie as [ROWS][128 bytes] with a row's eight 16-byte chunks permuted by the row
+// (reads of one chunk of 8 rows fall in different banks); the others as
+// [k][ROWS] with pairs of chunks permuted by k, for the transposing reads.
+template <typename T, bool TR, int ROWS> struct Tile {
+  static constexpr int EPC = 16 / (int)sizeof(T), BK = 128 / (int)sizeof(T);
+  static constexpr int CPR = TR ? ROWS / EPC : 8;  // chunks of a stored row
+  static constexpr int BYTES = ROWS * 128, CHUNKS = ROWS * 8;
+  // the source chunk that LDS slot s of stored row `row` holds (an involution)
+  static __device__ __forceinline__ int swap(int row, int s) {
+    if constexpr (!TR) return s ^ (row & 7);
+    else if constexpr (sizeof(T) == 4) return s;
+    else return s ^ (ROWS >= 128 ? 2 * (row & 7) : ROWS == 64 ? 2 * ((row >> 1) & 3) : 2 * ((row >> 2) & 1));
+  }
+  // rows 32 blk .. + 31, reduction elements 16 ks .. + 15: lane (c, g) holds
+  // row c, elements 8 g .. + 7
+  static __device__ __forceinline__ typename Frag<T>::type frag(const char* buf, int blk, int ks) {
+    const int lane = lane_id(), g = lane >> 5, c = lane & 31;
+    if constexpr (!TR && sizeof(T) == 2) {
+      const int row = 32 * blk + c;
+      return load_frag(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 2 * ks + g) * 16));
+    } else if constexpr (!TR) {
+      const int row = 32 * blk + c;
+      return join<T>(load_half(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 4 * ks + 2 * g) * 16)),
+                     load_half(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 4 * ks + 2 * g + 1) * 16)));
+    } else if constexpr (sizeof(T) == 2) {
+      const int i16 = lane & 15, k = 16 * ks + 8 * g + (i16 >> 2);
+      const int s = 4 * blk + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+      return lds_tr_frag(buf + k * ROWS * 2 + swap(k, s) * 16 + 8 * (i16 & 1),
+                         buf + (k + 4) * ROWS * 2 + swap(k + 4, s) * 16 + 8 * (i16 & 1));
+    } else {
+      const T* p = reinterpret_cast<const T*>(buf) + (16 * ks + 8 * g) * ROWS + 32 * blk + c;
+      typename Frag<T>::type f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = p[j * ROWS];
+      return f;
+    }
+  }
+};
+
+// One 16-byte chunk of an operand with `rows` rows and reduction length kend,
+// zeros outside; by elements where rows of the array are not whole chunks.
+template <typename T, bool TR>
+__device__ __forceinline__ f32x4 guarded_chunk(const T* src, int64_t ld, int64_t rows, int64_t kend, int64_t row, int64_t k,
+                                               bool whole) {
+  constexpr int EPC = 16 / (int)sizeof(T);
+  // stored row and column, and their ends
+  const int64_t sr = TR ? k : row, sc = TR ? row : k, re = TR ? kend : rows, ce = TR ? rows : kend;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (sr >= re) return v;
+  const T* s = src + sr * ld + sc;
+  if (whole) {
+    if (sc < ce) v = *reinterpret_cast<const f32x4*>(s);
+    return v;
+  }
+  T e[EPC];
+#pragma unroll
+  for (int j = 0; j < EPC; ++j) e[j] = sc + j < ce ? s[j] : from_f32<T>(0.f);
+  __builtin_memcpy(&v, e, 16);
+  return v;
+}
+
+// ---- epilogue ---------------------------------------------------------------------
+// Four consecutive outputs q .. q + 3 of row p: bias, activation, residual;
+// the pre-activation's values stay in y.
+template <typename T>
+__device__ __forceinline__ void finish(float (&y)[4], float (&o)[4], const LinGemmParams& p, int64_t row, int64_t q, bool whole) {
+  const T* bias = static_cast<const T*>(p.bias);
+  const T* res = static_cast<const T*>(p.res);
+  float b[4] = {0.f, 0.f, 0.f, 0.f}, r[4] = {0.f, 0.f, 0.f, 0.f};
+  if (whole) {
+    if (bias) {
+      const auto v = load_half(bias + q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b[e] = to_f32(v[e]);
+    }
+    if (res) {
+      const auto v = load_half(res + row * p.Q + q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r[e] = to_f32(v[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (q + e < p.Q) {
+        if (bias) b[e] = to_f32(bias[q + e]);
+        if (res) r[e] = to_f32(res[row * p.Q + q + e]);
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (bias) y[e] += b[e];
+    o[e] = activate(y[e], p.act);
+    if (res) o[e] += r[e];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_part(T* out, int64_t Q, int64_t row, int64_t q, const float (&v)[4], bool whole) {
+  if (whole) {
+    store4(out + row * Q + q, v[0], v[1], v[2], v[3]);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (q + e < Q) out[row * Q + q + e] = from_f32<T>(v[e]);
+}
+
+// ---- the product -------------------------------------------------------------------
+template <typename T, int PROD, bool LO, int BP, int BQ, int WP, int WQ, bool DIRECT, int NBUF>
+__global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
+  constexpr bool LT = lin_l_t(PROD), RT = lin_r_t(PROD);
+  using L = Tile<T, LT, BP>;
+  using R = Tile<T, RT, BQ>;
+  constexpr int EPC = L::EPC, BK = L::BK, NP = BP / WP / 32, NQ = BQ / WQ / 32, NW = WP * WQ, NT = 64 * NW;
+  constexpr int BUF = L::BYTES + R::BYTES * (LO ? 2 : 1);
+  __shared__ __attribute__((aligned(16))) char smem[BUF * NBUF];
+  const int lane = lane_id(), wave = wave_id(), g = lane >> 5, c = lane & 31;
+  const int wp = wave / WQ, wq = wave % WQ;
+
+  // tiles in the order q, p, split; the workgroups of one XCD (dealt out in
+  // turn) take a run of them, so they share the rows of L and R in its L2
+  const int64_t ntp = (p.P + BP - 1) / BP, ntq = (p.Q + BQ - 1) / BQ, total = ntp * ntq * p.splits;
+  const int64_t per = (total + 7) / 8, tile = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if ((int64_t)(blockIdx.x >> 3) >= per || tile >= total) return;  // whole workgroup, before any barrier
+  const int64_t q0 = tile % ntq * BQ, p0 = tile / ntq % ntp * BP;
+  const int z = (int)(tile / (ntq * ntp));
+  const int64_t k0 = z * p.kchunk, k1 = min(p.K, k0 + p.kchunk);
+  const int nsteps = (int)((k1 - k0 + BK - 1) / BK);
+  const int64_t lld = LT ? p.P : p.K, rld = RT ? p.Q : p.K;
+  const T* lsrc = static_cast<const T*>(p.l);
+  const T* rsrc = static_cast<const T*>(p.r);
+  const T* rlo = static_cast<const T*>(p.r_lo);
+
+  f32x16 acc[NQ][NP];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i)
+#pragma unroll
+    for (int j = 0; j < NP; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  auto compute = [&](const char* buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int ks = 0; ks < BK / 16; ++ks) {
+      typename Frag<T>::type lf[NP], rf[NQ];
+#pragma unroll
+      for (int j = 0; j < NP; ++j) lf[j] = L::frag(buf, wp * NP + j, ks);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) rf[i] = R::frag(buf + L::BYTES, wq * NQ + i, ks);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+#pragma unroll
+        for (int j = 0; j < NP; ++j) mma(acc[i][j], rf[i], lf[j]);
+      if constexpr (LO) {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) rf[i] = R::frag(buf + L::BYTES + R::BYTES, wq * NQ + i, ks);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+          for (int j = 0; j < NP; ++j) mma(acc[i][j], rf[i], lf[j]);
+      }
+    }
+  };
+
+  if constexpr (DIRECT) {
+    constexpr int IPW = BUF / 1024 / NW;  // 1 KiB copies of a step per wave
+    static_assert(BUF % (1024 * NW) == 0, "whole copies per wave");
+    // rows and columns past the end repeat the last ones: their products are
+    // not stored, and reduction rows past the end are cleared below
+    auto issue = [&](int s) __attribute__((always_inline)) {
+      if (s >= nsteps) return;
+      char* dst = smem + s % NBUF * BUF;
+      const int64_t k = k0 + (int64_t)s * BK;
+#pragma unroll
+      for (int u = 0; u < IPW; ++u) {
+        const int kib = wave * IPW + u;
+        const T* src;
+        if (kib < L::BYTES / 1024) {
+          const int e = kib * 64 + lane, row = e / L::CPR, ch = L::swap(row, e % L::CPR);
+          if constexpr (LT) src = lsrc + min(k + row, p.K - 1) * lld + min(p0 + (int64_t)ch * EPC, p.P - EPC);
+          else src = lsrc + min(p0 + row, p.P - 1) * lld + k + ch * EPC;
+        } else {
+          const int e0 = (kib - L::BYTES / 1024) * 64 + lane;
+          const bool lo = LO && e0 >= R::CHUNKS;
+          const int e = lo ? e0 - R::CHUNKS : e0, row = e / R::CPR, ch = R::swap(row, e % R::CPR);
+          const T* base = lo ? rlo : rsrc;
+          if constexpr (RT) src = base + min(k + row, p.K - 1) * rld + min(q0 + (int64_t)ch * EPC, p.Q - EPC);
+          else src = base + min(q0 + row, p.Q - 1) * rld + k + ch * EPC;
+        }
+        lds_copy16(src, dst + kib * 1024);
+      }
+    };
+    for (int s = 0; s < NBUF - 1; ++s) issue(s);
+    for (int s = 0; s < nsteps; ++s) {
+      // step s has landed: at most the NBUF - 2 steps after it are in flight
+      if (s + NBUF - 2 < nsteps) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(IPW * (NBUF - 2)) : "memory");
+      else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      lds_barrier();
+      issue(s + NBUF - 1);  // into the buffer of step s - 1, which every wave has left
+      char* buf = smem + s % NBUF * BUF;
+      if constexpr (LT && RT) {
+        const int left = (int)min((int64_t)BK, k1 - k0 - (int64_t)s * BK);
+        if (left < BK) {  // reduction rows past the end count as zero
+          for (int e = threadIdx.x; e < BUF / 16; e += NT) {
+            const int rr = e < L::CHUNKS ? e / L::CPR : (e - L::CHUNKS) % R::CHUNKS / R::CPR;
+            if (rr >= left) reinterpret_cast<f32x4*>(buf)[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+          __syncthreads();
+        }
+      }
+      compute(buf);
+    }
+  } else {
+    static_assert(NBUF == 2, "one step ahead in registers");
+    constexpr int NL = (L::CHUNKS + NT - 1) / NT, NR = (BUF / 16 - L::CHUNKS + NT - 1) / NT;
+    const bool lwhole = lld % EPC == 0, rwhole = rld % EPC == 0;
+    f32x4 lv[NL], rv[NR];
+    auto load = [&](int s) __attribute__((always_inline)) {
+      const int64_t k = k0 + (int64_t)s * BK;
+#pragma unroll
+      for (int u = 0; u < NL; ++u) {
+        const int e = u * NT + threadIdx.x, row = e / L::CPR, ch = L::swap(row, e % L::CPR);
+        if (e >= L::CHUNKS) continue;
+        lv[u] = LT ? guarded_chunk<T, true>(lsrc, lld, p.P, k1, p0 + ch * EPC, k + row, lwhole)
+                   : guarded_chunk<T, false>(lsrc, lld, p.P, k1, p0 + row, k + ch * EPC, lwhole);
+      }
+#pragma unroll
+      for (int u = 0; u < NR; ++u) {
+        const int e0 = u * NT + threadIdx.x;
+        const bool lo = LO && e0 >= R::CHUNKS;
+        const int e = lo ? e0 - R::CHUNKS : e0, row = e / R::CPR, ch = R::swap(row, e % R::CPR);
+        if (e >= R::CHUNKS) continue;
+        const T* base = lo ? rlo : rsrc;
+        rv[u] = RT ? guarded_chunk<T, true>(base, rld, p.Q, k1, q0 + ch * EPC, k + row, rwhole)
+                   : guarded_chunk<T, false>(base, rld, p.Q, k1, q0 + row, k + ch * EPC, rwhole);
+      }
+    };
+    load(0);
+    for (int s = 0; s < nsteps; ++s) {
+      char* buf = smem + (s & 1) * BUF;
+#pragma unroll
+      for (int u = 0; u < NL; ++u) {
+        const int e = u * NT + threadIdx.x;
+        if (e < L::CHUNKS) reinterpret_cast<f32x4*>(buf)[e] = lv[u];
+      }
+#pragma unroll
+      for (int u = 0; u < NR; ++u) {
+        const int e = u * NT + threadIdx.x;
+        if (e < BUF / 16 - L::CHUNKS) reinterpret_cast<f32x4*>(buf + L::BYTES)[e] = rv[u];
+      }
+      lds_barrier();  // the buffer two steps on is written after the next barrier, when every wave has left this one
+      if (s + 1 < nsteps) load(s + 1);
+      compute(buf);
+    }
+  }
+
+  // lane (c, g) holds row p = c, outputs 8 u + 4 g .. + 3 of every block
+  const bool whole = p.Q % (p.part ? 4 : EPC) == 0;
+#pragma unroll
+  for (int j = 0; j < NP; ++j) {
+    const int64_t row = p0 + 32 * (wp * NP + j) + c;
+    const bool in = row < p.P;
+    const int64_t rr = min(row, p.P - 1);
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const int64_t qb = q0 + 32 * (wq * NQ + i);
+      if (qb >= p.Q) continue;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float y[2][4], o[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[h][e] = acc[i][j][8 * u + 4 * h + e];
+        if (p.part) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int64_t q = qb + 16 * u + 8 * h + 4 * g;
+            if (in && q < p.Q) store_part(p.part + z * p.part_stride, p.Q, row, q, y[h], whole);
+          }
+          continue;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int64_t q = qb + 16 * u + 8 * h + 4 * g;
+          if (q < p.Q) finish<T>(y[h], o[h], p, rr, q, whole);
+          else o[h][0] = o[h][1] = o[h][2] = o[h][3] = 0.f;
+        }
+        if (whole && sizeof(T) == 2) {
+          // runs of 8 outputs per lane
+          const int64_t q = qb + 16 * u + 8 * g;
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = o[e / 4][e % 4];
+          bf16x8 w;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = (__bf16)v[e];
+          w = runs_of_8(w);
+          if (in && q < p.Q) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out) + row * p.Q + q) = w;
+          if (p.pre) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = (__bf16)y[e / 4][e % 4];
+            w = runs_of_8(w);
+            if (in && q < p.Q) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.pre) + row * p.Q + q) = w;
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int64_t q = qb + 16 * u + 8 * h + 4 * g;
+            if (in && q < p.Q) {
+              store_part(static_cast<T*>(p.out), p.Q, row, q, o[h], whole);
+              if (p.pre) store_part(static_cast<T*>(p.pre), p.Q, row, q, y[h], whole);
+            }
+          }
+        }
+      }
+    }
+  }
+}
+
+// ---- epilogue of a product whose reduction was split ----------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void k_linear_finish(LinGemmParams p) {
+  const int64_t nq = (p.Q + 3) / 4, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= p.P * nq) return;
+  const int64_t row = i / nq, q = i % nq * 4;
+  const bool whole = p.Q % 4 == 0;
+  float y[4] = {0.f, 0.f, 0.f, 0.f}, o[4];
+  for (int z = 0; z < p.splits; ++z) {
+    const float* s = p.part + z * p.part_stride + row * p.Q + q;
+    if (whole) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(s);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += v[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (q + e < p.Q) y[e] += s[e];
+    }
+  }
+  finish<T>(y, o, p, row, q, whole);
+  store_part(static_cast<T*>(p.out), p.Q, row, q, o, whole);
+  if (p.pre) store_part(static_cast<T*>(p.pre), p.Q, row, q, y, whole);
+}
+
+// ---- dP = dOut * act'(pre) and its column sums --------------------------------------------
+// A workgroup takes a chunk of rows and a strip of columns: VEC (16 bytes) or
+// one column per lane, CL lanes across, 256 / CL rows at a time.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void k_linear_slope(LinSlopeParams p, int cl_log2) {
+  __shared__ float sums[256 * VEC];
+  const int cl = 1 << cl_log2, lc = threadIdx.x & (cl - 1), lr = threadIdx.x >> cl_log2, rl = 256 >> cl_log2;
+  const int64_t col = ((int64_t)blockIdx.y * cl + lc) * VEC;
+  const int64_t r0 = (int64_t)blockIdx.x * p.chunk, r1 = min(p.T, r0 + p.chunk);
+  const T* d = static_cast<const T*>(p.dout);
+  const T* a = static_cast<const T*>(p.pre);
+  float s[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+  if (col < p.N) {
+    for (int64_t r = r0 + lr; r < r1; r += rl) {
+      const int64_t at = r * p.N + col;
+      T dv[VEC], av[VEC], hi[VEC], lo[VEC];
+      __builtin_memcpy(dv, __builtin_assume_aligned(d + at, VEC * sizeof(T)), VEC * sizeof(T));
+      if (p.act != kActNone) __builtin_memcpy(av, __builtin_assume_aligned(a + at, VEC * sizeof(T)), VEC * sizeof(T));
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        float v = to_f32(dv[e]);
+        if (p.act != kActNone) v *= slope(to_f32(av[e]), p.act);
+        s[e] += v;
+        hi[e] = from_f32<T>(v);
+        lo[e] = from_f32<T>(v - to_f32(hi[e]));
+      }
+      if (p.dp) __builtin_memcpy(__builtin_assume_aligned(static_cast<T*>(p.dp) + at, VEC * sizeof(T)), hi, VEC * sizeof(T));
+      if (p.dp_lo) __builtin_memcpy(__builtin_assume_aligned(static_cast<T*>(p.dp_lo) + at, VEC * sizeof(T)), lo, VEC * sizeof(T));
+    }
+  }
+  if (!p.part) return;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sums[(lr * cl + lc) * VEC + e] = s[e];
+  for (int h = rl / 2; h > 0; h /= 2) {
+    __syncthreads();
+    if (lr < h)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sums[(lr * cl + lc) * VEC + e] += sums[((lr + h) * cl + lc) * VEC + e];
+  }
+  if (lr == 0 && col < p.N)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) p.part[blockIdx.x * p.part_ld + col + e] = sums[lc * VEC + e];
+}
+
+// ---- sums of partials in a fixed order ---------------------------------------------------
+// 64 outputs per workgroup, four waves that each sum a run of the splits.
+__global__ __launch_bounds__(256) void k_linear_sum(LinSumParams p, int64_t first1) {
+  __shared__ float sums[4][64];
+  const int jb = p.njobs > 1 && (int64_t)blockIdx.x >= first1 ? 1 : 0;
+  const LinSumJob& j = p.job[jb];
+  const int lane = lane_id(), wave = wave_id();
+  const int64_t i = ((int64_t)blockIdx.x - (jb ? first1 : 0)) * 64 + lane;
+  const int per = (j.splits + 3) / 4, s0 = wave * per, s1 = min(j.splits, s0 + per);
+  float s = 0.f;
+  if (i < j.n) {
+    const float* x = j.part + i;
+    int z = s0;
+    for (; z + 8 <= s1; z += 8) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = x[(z + e) * j.stride];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += v[e];
+    }
+    for (; z < s1; ++z) s += x[z * j.stride];
+  }
+  sums[wave][lane] = s;
+  __syncthreads();
+  if (wave == 0 && i < j.n) j.out[i] = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+}
+
+template <typename T, int PROD, bool LO, int BP, int BQ, int WP, int WQ, bool DIRECT, int NBUF>
+hipError_t launch_tile(const LinGemmParams& p, hipStream_t s) {
+  const int64_t total = (p.P + BP - 1) / BP * ((p.Q + BQ - 1) / BQ) * p.splits;
+  const int64_t grid = (total + 7) / 8 * 8;
+  k_linear<T, PROD, LO, BP, BQ, WP, WQ, DIRECT, NBUF><<<dim3((unsigned)grid), 64 * WP * WQ, 0, s>>>(p);
+  return hipGetLastError();
+}
+
+template <typename T, int PROD, bool LO>
+hipError_t launch_prod(const LinGemmParams& p, int tile, bool direct, hipStream_t s) {
+  switch (tile) {
+    case kTile128:
+      return direct ? launch_tile<T, PROD, LO, 128, 128, 2, 2, true, 2>(p, s) : launch_tile<T, PROD, LO, 128, 128, 2, 2, false, 2>(p, s);
+    case kTile64:
+      return direct ? launch_tile<T, PROD, LO, 64, 64, 2, 2, true, 3>(p, s) : launch_tile<T, PROD, LO, 64, 64, 2, 2, false, 2>(p, s);
+    case kTile128x32: return launch_tile<T, PROD, LO, 128, 32, 4, 1, false, 2>(p, s);
+    default: return launch_tile<T, PROD, LO, 32, 128, 1, 4, false, 2>(p, s);
+  }
+}
+
+}  // namespace
+
+bool lin_direct(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K) {
+  const int64_t epc = 16 / elem_bytes, bk = lin_step(elem_bytes);
+  const bool lok = lin_l_t(prod) ? P % epc == 0 : K % bk == 0;
+  const bool rok = lin_r_t(prod) ? Q % epc == 0 : K % bk == 0;
+  return lok && rok;
+}
+
+template <typename T>
+hipError_t launch_lin_gemm(const LinGemmParams& p, int prod, int tile, bool direct, hipStream_t s) {
+  if (prod == kLinForward) return launch_prod<T, kLinForward, false>(p, tile, direct, s);
+  if (prod == kLinInput) return launch_prod<T, kLinInput, false>(p, tile, direct, s);
+  if constexpr (sizeof(T) == 2) {
+    if (p.r_lo) return launch_prod<T, kLinWeight, true>(p, tile, direct, s);
+  }
+  return launch_prod<T, kLinWeight, false>(p, tile, direct, s);
+}
+template hipError_t launch_lin_gemm<float>(const LinGemmParams&, int, int, bool, hipStream_t);
+template hipError_t launch_lin_gemm<__bf16>(const LinGemmParams&, int, int, bool, hipStream_t);
+
+template <typename T>
+hipError_t launch_lin_finish(const LinGemmParams& p, hipStream_t s) {
+  const int64_t n = p.P * ((p.Q + 3) / 4);
+  k_linear_finish<T><<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>(p);
+  return hipGetLastError();
+}
+template hipError_t launch_lin_finish<float>(const LinGemmParams&, hipStream_t);
+template hipError_t launch_lin_finish<__bf16>(const LinGemmParams&, hipStream_t);
+
+template <typename T>
+hipError_t launch_lin_slope(const LinSlopeParams& p, hipStream_t s) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const int vec = p.N % V == 0 ? V : 1;
+  int cl = 0;
+  while ((1 << cl) < (vec == 1 ? 256 : 32) && (int64_t)vec << cl < p.N) ++cl;
+  const dim3 grid((unsigned)p.nchunks, (unsigned)((p.N + ((int64_t)vec << cl) - 1) / ((int64_t)vec << cl)));
+  if (vec == 1) k_linear_slope<T, 1><<<grid, 256, 0, s>>>(p, cl);
+  else k_linear_slope<T, V><<<grid, 256, 0, s>>>(p, cl);
+  return hipGetLastError();
+}
+template hipError_t launch_lin_slope<float>(const LinSlopeParams&, hipStream_t);
+template hipError_t launch_lin_slope<__bf16>(const LinSlopeParams&, hipStream_t);
+
+hipError_t launch_lin_sum(const LinSumParams& p, hipStream_t s) {
+  const int64_t first1 = (p.job[0].n + 63) / 64, second = p.njobs > 1 ? (p.job[1].n + 63) / 64 : 0;
+  k_linear_sum<<<dim3((unsigned)(first1 + second)), 256, 0, s>>>(p, first1);
+  return hipGetLastError();
+}
+
+}  // namespace flarepp

@@ -7,6 +7,7 @@ stream.  If the library is missing this module raises; there is no fallback.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import operator
 import os
@@ -39,9 +40,21 @@ EXPORTS = (
     "flarepp_mixer_backward_shared", "flarepp_mixer_forward_train", "flarepp_mixer_backward_from_saved",
     "flarepp_block_backward_workspace_bytes", "flarepp_block_backward",
     "flarepp_mixer_noalloc_max_bytes", "flarepp_mixer_forward_noalloc",
+    "flarepp_linear_workspace_bytes", "flarepp_linear_forward",
+    "flarepp_linear_backward_workspace_bytes", "flarepp_linear_backward",
+    "flarepp_embedding_forward", "flarepp_embedding_backward_workspace_bytes", "flarepp_embedding_backward",
+    "flarepp_adamw_schedule", "flarepp_adamw_step",
 )
 PATH_UNFUSED = 0
 PATH_FUSED = 1
+ACT_NONE = 0
+ACT_RELU = 1
+ACT_GELU = 2
+ACT_SILU = 3
+STATE_F32 = 0
+STATE_E4M3 = 1
+ADAMW_BLOCK = 256  # elements that share a scale
+ADAMW_SCHEDULE_BYTES = 24
 PROFILE_EVENTS = 9
 PROFILE_STAGES = ("prep", "project", "call1_encode", "call1_combine", "call2_encode",
                   "call2_combine", "call3_decode", "merge")
@@ -53,6 +66,13 @@ class FlareppError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"flarepp error {code}: {msg}")
         self.code = code
+
+
+class _AdamwTensor(ctypes.Structure):
+    """flarepp_adamw_tensor of include/flarepp.h."""
+    _fields_ = [("n", ctypes.c_int64), ("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("p_low", ctypes.c_void_p), ("weight_decay", ctypes.c_double)]
 
 
 def load(path: str = LIB_PATH) -> ctypes.CDLL:
@@ -131,6 +151,25 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.flarepp_mixer_noalloc_max_bytes.argtypes = []
     lib.flarepp_mixer_forward_noalloc.restype = i32
     lib.flarepp_mixer_forward_noalloc.argtypes = [i32, i64, i64, i64, i64, i64] + [vp] * 8 + [vp]
+    lib.flarepp_linear_workspace_bytes.restype = sz
+    lib.flarepp_linear_workspace_bytes.argtypes = [i32, i64, i64, i64]
+    lib.flarepp_linear_forward.restype = i32
+    lib.flarepp_linear_forward.argtypes = [i32, i32, i64, i64, i64] + [vp] * 6 + [vp, sz, vp]
+    lib.flarepp_linear_backward_workspace_bytes.restype = sz
+    lib.flarepp_linear_backward_workspace_bytes.argtypes = [i32, i32, i64, i64, i64]
+    lib.flarepp_linear_backward.restype = i32
+    lib.flarepp_linear_backward.argtypes = [i32, i32, i64, i64, i64] + [vp] * 4 + [vp, fp, fp] + [vp, sz, vp]
+    lib.flarepp_embedding_forward.restype = i32
+    lib.flarepp_embedding_forward.argtypes = [i32, i64, i64, i64, vp, vp, ctypes.c_float, vp, vp]
+    lib.flarepp_embedding_backward_workspace_bytes.restype = sz
+    lib.flarepp_embedding_backward_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.flarepp_embedding_backward.restype = i32
+    lib.flarepp_embedding_backward.argtypes = [i32, i64, i64, i64, vp, vp, ctypes.c_float, fp, vp, sz, vp]
+    f64 = ctypes.c_double
+    lib.flarepp_adamw_schedule.restype = i32
+    lib.flarepp_adamw_schedule.argtypes = [f64, f64, f64, i64, vp]
+    lib.flarepp_adamw_step.restype = i32
+    lib.flarepp_adamw_step.argtypes = [i32, i64, ctypes.POINTER(_AdamwTensor), f64, f64, f64, f64, i64, vp, vp]
     _lib = lib
     return lib
 
@@ -640,6 +679,262 @@ def flarepp_block_backward(X, gamma, beta, Wk, Wv, Wkt, Wvt, Wo, seeds, dO, *, H
     return g
 
 
+# ---------------------------------------------------------------------------
+# operators around the mixer: linear layer, embedding, optimiser step
+# ---------------------------------------------------------------------------
+
+def _on_device(device: torch.device):
+    """Context in which ``device`` is the current one, as launches need."""
+    return torch.cuda.device(device) if device.type == "cuda" else contextlib.nullcontext()
+
+
+def _layer(X, W):
+    """(T, K, N) of a linear layer's X [..., K] and W [K, N]."""
+    for name, t in (("X", X), ("W", W)):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
+    _dtype_code(X)
+    if X.dim() < 1 or W.dim() != 2:
+        raise ValueError(f"X must be [..., K] and W [K, N], got {tuple(X.shape)} and {tuple(W.shape)}")
+    K, N = X.shape[-1], W.shape[1]
+    _same(W, "W", (K, N), X.dtype, X.device)
+    T = 1
+    for n in X.shape[:-1]:
+        T *= n
+    return T, K, N
+
+
+def _act(act) -> int:
+    try:
+        return operator.index(act)
+    except TypeError:
+        raise TypeError(f"act must be one of the ACT_ constants, got {act!r}") from None
+
+
+def _check_ws(ws, device) -> None:
+    if ws is None:
+        return
+    if not isinstance(ws, torch.Tensor) or ws.dtype != torch.uint8:
+        raise TypeError("ws must be a uint8 torch.Tensor")
+    if ws.device != device:
+        raise ValueError(f"ws is on {ws.device}, expected {device}")
+
+
+def flarepp_linear_workspace_bytes(dtype: int, T: int, K: int, N: int) -> int:
+    return int(load().flarepp_linear_workspace_bytes(dtype, T, K, N))
+
+
+def flarepp_linear_forward(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None, *, act: int = ACT_NONE,
+                           residual: Optional[torch.Tensor] = None, keep_pre: bool = False,
+                           out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """out = residual + act(X W + bias), X [..., K], W [K, N], all in X's
+    dtype.  With ``keep_pre`` returns (out, pre): the pre-activation that
+    flarepp_linear_backward needs.  ``out`` may be ``residual``."""
+    lib = load()
+    T, K, N = _layer(X, W)
+    act = _act(act)
+    shape = X.shape[:-1] + (N,)
+    if bias is not None:
+        _same(bias, "bias", (N,), X.dtype, X.device)
+    for name, t in (("residual", residual), ("out", out)):
+        if t is not None:
+            _same(t, name, shape, X.dtype, X.device)
+    _check_ws(ws, X.device)
+    dt = _dtype_code(X)
+    O = out if out is not None else torch.empty(shape, dtype=X.dtype, device=X.device)
+    pre = torch.empty(shape, dtype=X.dtype, device=X.device) if keep_pre else None
+    w = _workspace(flarepp_linear_workspace_bytes(dt, T, K, N), X.device, ws)
+    with _on_device(X.device):
+        rc = lib.flarepp_linear_forward(dt, act, T, K, N, _ptr(X), _ptr(W), _ptr(bias), _ptr(residual), _ptr(O), _ptr(pre),
+                                        _ptr(w), w.numel(), _stream(X.device))
+    _check(rc)
+    return (O, pre) if keep_pre else O
+
+
+def flarepp_linear_backward_workspace_bytes(dtype: int, act: int, T: int, K: int, N: int) -> int:
+    return int(load().flarepp_linear_backward_workspace_bytes(dtype, act, T, K, N))
+
+
+def flarepp_linear_backward(X: torch.Tensor, W: torch.Tensor, dOut: torch.Tensor, *, pre: Optional[torch.Tensor] = None,
+                            act: int = ACT_NONE, want_dX: bool = True, want_dW: bool = True, want_dbias: bool = True,
+                            ws: Optional[torch.Tensor] = None, out: Optional[dict] = None):
+    """Gradients of <out, dOut> for the linear layer: a dict of dX [..., K] (X's
+    dtype), dW [K, N] and dbias [N] (fp32), those wanted (written into
+    ``out``'s tensors when given: then those that it has).  ``pre`` is what the
+    forward kept; ACT_NONE needs none.  The residual's gradient is dOut."""
+    lib = load()
+    T, K, N = _layer(X, W)
+    act = _act(act)
+    _same(dOut, "dOut", X.shape[:-1] + (N,), X.dtype, X.device)
+    if pre is not None:
+        _same(pre, "pre", dOut.shape, X.dtype, X.device)
+    _check_ws(ws, X.device)
+    forms = {"dX": (X.shape, X.dtype), "dW": ((K, N), torch.float32), "dbias": ((N,), torch.float32)}
+    if out is not None:
+        unknown = set(out) - set(forms)
+        if unknown:
+            raise ValueError(f"out has unknown entries {sorted(unknown)}")
+        for k, t in out.items():
+            _same(t, f"out[{k!r}]", *forms[k], X.device)
+        g = dict(out)
+    else:
+        g = {k: torch.empty(shape, dtype=dtype, device=X.device) for (k, (shape, dtype)), want
+             in zip(forms.items(), (want_dX, want_dW, want_dbias)) if want}
+    dt = _dtype_code(X)
+    w = _workspace(flarepp_linear_backward_workspace_bytes(dt, act, T, K, N), X.device, ws)
+    with _on_device(X.device):
+        rc = lib.flarepp_linear_backward(dt, act, T, K, N, _ptr(X), _ptr(W), _ptr(pre), _ptr(dOut),
+                                         *[_ptr(g.get(k)) for k in forms], _ptr(w), w.numel(), _stream(X.device))
+    _check(rc)
+    return g
+
+
+def _ids(ids):
+    if not isinstance(ids, torch.Tensor):
+        raise TypeError(f"ids must be a torch.Tensor, got {type(ids).__name__}")
+    if ids.dtype != torch.int64:
+        raise TypeError(f"ids has dtype {ids.dtype}, expected torch.int64")
+
+
+def flarepp_embedding_forward(ids: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0,
+                              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[...] = scale * table[ids[...]]: ids (int64) of any shape, table
+    [V, C], out ids.shape + (C,) in the table's dtype.  Rows of negative ids
+    (padding) are zero, rows of ids >= V NaN."""
+    lib = load()
+    _ids(ids)
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must be a [V, C] tensor")
+    dt = _dtype_code(table)
+    if ids.device != table.device:
+        raise ValueError(f"ids is on {ids.device}, expected {table.device} (the device of table)")
+    V, C = table.shape
+    shape = ids.shape + (C,)
+    if out is not None:
+        _same(out, "out", shape, table.dtype, table.device)
+    O = out if out is not None else torch.empty(shape, dtype=table.dtype, device=table.device)
+    with _on_device(table.device):
+        rc = lib.flarepp_embedding_forward(dt, ids.numel(), V, C, _ptr(ids), _ptr(table), float(scale), _ptr(O),
+                                           _stream(table.device))
+    _check(rc)
+    return O
+
+
+def flarepp_embedding_backward_workspace_bytes(T: int, V: int, C: int) -> int:
+    return int(load().flarepp_embedding_backward_workspace_bytes(T, V, C))
+
+
+def flarepp_embedding_backward(ids: torch.Tensor, dOut: torch.Tensor, *, V: int, scale: float = 1.0,
+                               out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dTable [V, C] (fp32) of the embedding of ``ids``: scale * the sums of
+    dOut (ids.shape + (C,), float32 or bfloat16) over the positions of every
+    symbol.  Ids outside [0, V) take no gradient."""
+    lib = load()
+    _ids(ids)
+    if not isinstance(dOut, torch.Tensor) or dOut.dim() != ids.dim() + 1:
+        raise ValueError("dOut must be a tensor of shape ids.shape + (C,)")
+    dt = _dtype_code(dOut)
+    C = dOut.shape[-1]
+    _same(dOut, "dOut", ids.shape + (C,), dOut.dtype, ids.device)
+    try:
+        V = operator.index(V)
+    except TypeError:
+        raise TypeError(f"V must be an integer, got {type(V).__name__}") from None
+    if out is not None:
+        _same(out, "out", (V, C), torch.float32, ids.device)
+    _check_ws(ws, ids.device)
+    T = ids.numel()
+    need = flarepp_embedding_backward_workspace_bytes(T, V, C)
+    if not need:
+        _check(ERR_INVALID_ARG if min(T, V, C) < 1 else ERR_UNSUPPORTED)
+    g = out if out is not None else torch.empty((V, C), dtype=torch.float32, device=ids.device)
+    w = _workspace(need, ids.device, ws)
+    with _on_device(ids.device):
+        rc = lib.flarepp_embedding_backward(dt, T, V, C, _ptr(ids), _ptr(dOut), float(scale), _ptr(g), _ptr(w), w.numel(),
+                                            _stream(ids.device))
+    _check(rc)
+    return g
+
+
+class AdamwPlan:
+    """The checked table of a step's tensors (flarepp_adamw_plan).  It keeps
+    the tensors' memory alive; a program makes it once and again only when one
+    of them is replaced."""
+
+    def __init__(self, state: int, tensors, table, device):
+        self.state, self.tensors, self.table, self.device = state, tensors, table, device
+
+
+def flarepp_adamw_plan(tensors) -> AdamwPlan:
+    """Check and lay out the tensors of flarepp_adamw_step: dicts with p, g
+    (float32, any shape), m, v (p's shape; float32, or float8_e4m3fn with
+    m_scale, v_scale float32 [ceil(n / 256)], then for every tensor), optionally
+    p_low (bfloat16, p's shape) and weight_decay.  Entries may be None."""
+    tensors = list(tensors)
+    if not tensors:
+        raise ValueError("tensors is empty")
+    table = (_AdamwTensor * len(tensors))()
+    kept, state, device = [], None, None
+    for i, t in enumerate(tensors):
+        p = t.get("p")
+        if not isinstance(p, torch.Tensor):
+            raise TypeError(f"tensor {i}: p must be a torch.Tensor, got {type(p).__name__}")
+        unknown = set(t) - {"p", "g", "m", "v", "m_scale", "v_scale", "p_low", "weight_decay"}
+        if unknown:
+            raise ValueError(f"tensor {i} has unknown entries {sorted(unknown)}")
+        m = t.get("m")
+        if not isinstance(m, torch.Tensor) or m.dtype not in (torch.float32, torch.float8_e4m3fn):
+            raise TypeError(f"tensor {i}: m must be a float32 or float8_e4m3fn tensor")
+        mine = STATE_F32 if m.dtype == torch.float32 else STATE_E4M3
+        state, device = (mine, p.device) if state is None else (state, device)
+        if mine != state:
+            raise ValueError(f"tensor {i}: the state is float32 or float8_e4m3fn for every tensor alike")
+        f32, n = torch.float32, p.numel()
+        forms = {"p": (p.shape, f32), "g": (p.shape, f32), "m": (p.shape, m.dtype), "v": (p.shape, m.dtype)}
+        if state == STATE_E4M3:
+            forms["m_scale"] = forms["v_scale"] = ((-(-n // ADAMW_BLOCK),), f32)
+        elif t.get("m_scale") is not None or t.get("v_scale") is not None:
+            raise ValueError(f"tensor {i}: a float32 state has no scales")
+        if t.get("p_low") is not None:
+            forms["p_low"] = (p.shape, torch.bfloat16)
+        row, alive = table[i], {}
+        row.n, row.weight_decay = n, float(t.get("weight_decay") or 0.0)
+        for k, (shape, dtype) in forms.items():
+            _same(t.get(k), f"tensor {i}: {k}", shape, dtype, device)
+        for k in forms:
+            alive[k] = t[k].detach()  # this memory, whatever becomes of the caller's tensor
+            setattr(row, k, _ptr(alive[k]).value)
+        kept.append(alive)
+    return AdamwPlan(state, kept, table, device)
+
+
+def flarepp_adamw_schedule(*, lr: float, step: int, betas=(0.9, 0.999), out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """What changes from step to step, as a uint8 [24] host tensor: copied to a
+    device tensor that flarepp_adamw_step was given as ``schedule``, it sets lr
+    and step of the replays that follow."""
+    lib = load()
+    s = torch.empty(ADAMW_SCHEDULE_BYTES, dtype=torch.uint8) if out is None else out
+    _same(s, "out", (ADAMW_SCHEDULE_BYTES,), torch.uint8, torch.device("cpu"))
+    _check(lib.flarepp_adamw_schedule(lr, betas[0], betas[1], step, ctypes.c_void_p(s.data_ptr())))
+    return s
+
+
+def flarepp_adamw_step(plan: AdamwPlan, *, lr: float, step: int, betas=(0.9, 0.999), eps: float = 1e-8,
+                       schedule: Optional[torch.Tensor] = None) -> None:
+    """AdamW step number ``step`` (from 1) on the plan's tensors, in place.
+    With ``schedule`` (a device copy of flarepp_adamw_schedule's tensor) lr and
+    step are read from it when the work runs, as a captured step needs."""
+    lib = load()
+    if not isinstance(plan, AdamwPlan):
+        raise TypeError(f"plan must come from flarepp_adamw_plan, got {type(plan).__name__}")
+    if schedule is not None:
+        _same(schedule, "schedule", (ADAMW_SCHEDULE_BYTES,), torch.uint8, plan.device)
+    with _on_device(plan.device):
+        rc = lib.flarepp_adamw_step(plan.state, len(plan.table), plan.table, lr, betas[0], betas[1], eps, step,
+                                    _ptr(schedule), _stream(plan.device))
+    _check(rc)
+
+
 # short aliases
 project = flarepp_project
 route = flarepp_route
@@ -656,3 +951,10 @@ mixer_backward_shared = flarepp_mixer_backward_shared
 mixer_forward_train = flarepp_mixer_forward_train
 mixer_backward_from_saved = flarepp_mixer_backward_from_saved
 block_backward = flarepp_block_backward
+linear_forward = flarepp_linear_forward
+linear_backward = flarepp_linear_backward
+embedding_forward = flarepp_embedding_forward
+embedding_backward = flarepp_embedding_backward
+adamw_plan = flarepp_adamw_plan
+adamw_schedule = flarepp_adamw_schedule
+adamw_step = flarepp_adamw_step

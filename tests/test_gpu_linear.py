@@ -1,0 +1,245 @@
+"""The linear layer and its gradients against the float64 reference.
+
+Tolerances, per element.  A sum of n fp32 products is off by at most n 2^-24
+times the sum of their magnitudes (S).  GELU and SiLU have slopes below 1.13,
+GELU's normal distribution (a published approximation, 1.5e-7 in erf, and
+fp32 operations) is off by less than 4e-7, SiLU's sigmoid by less than 4e-7.
+A rounding to the storage type is off by half a step: 2^-8 (bf16) or 2^-24
+(fp32) of the value.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import layers_oracle as orc
+from paper_2608_11519_amd import flarepp as fp
+
+pytestmark = pytest.mark.gpu
+
+ACTS = {"none": fp.ACT_NONE, "relu": fp.ACT_RELU, "gelu": fp.ACT_GELU, "silu": fp.ACT_SILU}
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+# one to many rows; widths of one element, odd ones, below and above a tile,
+# multiples of a step; long reductions that are split; narrow outputs and inputs
+SHAPES = [(1, 1, 1), (1, 128, 256), (2, 7, 5), (3, 64, 32), (33, 64, 64), (65, 65, 63), (64, 128, 64), (130, 100, 10),
+          (127, 3, 128), (257, 96, 31), (1000, 128, 256), (40, 1000, 300), (64, 2048, 64), (5, 1024, 1000), (5000, 64, 4),
+          (300, 520, 72), (129, 136, 129), (16385, 64, 256)]
+
+
+def _f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _inputs(T, K, N, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    rn = lambda *s: torch.randn(*s, generator=g).to(DT[dtype]).cuda()  # noqa: E731
+    return rn(T, K), (torch.randn(K, N, generator=g) / K ** 0.5).to(DT[dtype]).cuda(), rn(N), rn(T, N), rn(T, N)
+
+
+def _within(name, got, ref, tol):
+    got = _f64(got)
+    assert got.shape == ref.shape
+    assert np.isfinite(got).all(), name
+    worst = np.max(np.abs(got - ref) / tol)
+    print(f"  {name}: {worst:.3f} of the tolerance", flush=True)
+    assert worst <= 1.0, (name, worst)
+
+
+def _check_forward(X, W, b, r, act, dtype, out, pre):
+    x, w = _f64(X), _f64(W)
+    ref, y = orc.linear_forward(x, w, None if b is None else _f64(b), None if r is None else _f64(r), act)
+    S = np.abs(x) @ np.abs(w) + (0 if b is None else np.abs(_f64(b)))
+    n = X.shape[1] + 4
+    err = n * 2.0 ** -24 * S
+    if pre is not None:
+        _within("pre", pre, y, err * (1 + HALF[dtype]) + HALF[dtype] * np.abs(y) + 1e-30)
+    err = 1.13 * err + 4e-7 * np.abs(y) + 2.0 ** -23 * np.abs(ref)
+    if r is not None:
+        err = err + 2.0 ** -23 * np.abs(_f64(r))
+    _within("out", out, ref, err * (1 + HALF[dtype]) + HALF[dtype] * np.abs(ref) + 1e-30)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_forward(shape, dtype):
+    T, K, N = shape
+    X, W, b, r, _ = _inputs(T, K, N, dtype)
+    _check_forward(X, W, b, r, "gelu", dtype, *fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, residual=r, keep_pre=True))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("parts", ["", "b", "r", "br"])
+@pytest.mark.parametrize("shape", [(70, 64, 136), (37, 1100, 9)], ids=str)
+def test_epilogues(shape, parts, act, dtype):
+    X, W, b, r, _ = _inputs(*shape, dtype, seed=1)
+    b, r = b if "b" in parts else None, r if "r" in parts else None
+    out = fp.flarepp_linear_forward(X, W, b, act=ACTS[act], residual=r)
+    _check_forward(X, W, b, r, act, dtype, out, None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_activations_over_their_range(dtype):
+    # W = 1: the pre-activations are the inputs, from the tails to the middle
+    y = torch.cat([torch.linspace(-40, 40, 4001), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 3e38, -3e38])]).to(DT[dtype]).cuda()
+    one = torch.ones(1, 1, dtype=DT[dtype], device="cuda")
+    for act in ACTS:
+        got = _f64(fp.flarepp_linear_forward(y[:, None], one, act=ACTS[act]))[:, 0]
+        with np.errstate(over="ignore"):
+            ref = orc.activate(_f64(y), act)
+        # y times a factor in [0, 1] that is off by less than 4e-7, then one rounding
+        off = 0.0 if act in ("none", "relu") else 4e-7 * np.abs(_f64(y))
+        assert np.all(np.abs(got - ref) <= (1 + HALF[dtype]) * off + HALF[dtype] * np.abs(ref) + 1e-44), act
+    special = torch.tensor([[float("nan")], [float("inf")]], dtype=DT[dtype], device="cuda")
+    for act in ACTS:
+        got = fp.flarepp_linear_forward(special, one, act=ACTS[act])
+        assert torch.isnan(got[0, 0]) and torch.isinf(got[1, 0]) and got[1, 0] > 0, act
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(65, 64, 72), (65, 40, 72), (65, 65, 63), (130, 64, 10)], ids=str)
+def test_reads_and_writes_nothing_outside(shape, dtype):
+    """Inputs end where NaN begin, and the outputs' surroundings stay."""
+    T, K, N = shape
+    pad = 4096
+
+    def inside(t, fill):
+        buf = torch.full((t.numel() + 2 * pad,), fill, dtype=t.dtype, device="cuda")
+        v = buf[pad:pad + t.numel()].view(t.shape)
+        v.copy_(t)
+        return buf, v
+
+    X, W, b, r, d = _inputs(T, K, N, dtype, seed=2)
+    (_, Xv), (_, Wv), (_, bv), (_, rv) = (inside(t, float("nan")) for t in (X, W, b, r))
+    obuf, ov = inside(torch.zeros_like(r), 7.0)
+    fp.flarepp_linear_forward(Xv, Wv, bv, act=fp.ACT_SILU, residual=rv, out=ov)
+    assert torch.equal(ov, fp.flarepp_linear_forward(X, W, b, act=fp.ACT_SILU, residual=r))
+    n = ov.numel()
+    assert (obuf[:pad] == 7).all() and (obuf[pad + n:] == 7).all()
+    _, dv = inside(d, float("nan"))
+    (_, pv) = inside(r, float("nan"))
+    outs = {"dX": inside(torch.zeros_like(X), 7.0), "dW": inside(torch.zeros(K, N, device="cuda"), 7.0),
+            "dbias": inside(torch.zeros(N, device="cuda"), 7.0)}
+    fp.flarepp_linear_backward(Xv, Wv, dv, pre=pv, act=fp.ACT_SILU, out={k: v[1] for k, v in outs.items()})
+    ref = fp.flarepp_linear_backward(X, W, d, pre=r, act=fp.ACT_SILU)
+    for k, (buf, v) in outs.items():
+        assert torch.equal(v, ref[k]) and torch.isfinite(v.float()).all(), k
+        assert (buf[:pad] == 7).all() and (buf[pad + v.numel():] == 7).all(), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(200, 64, 128), (33, 1030, 12)], ids=str)
+def test_a_row_that_is_not_finite_stays_in_its_row(shape, dtype):
+    X, W, b, _, _ = _inputs(*shape, dtype, seed=3)
+    ref = fp.flarepp_linear_forward(X, W, b)
+    bad = X.clone()
+    bad[7, 3], bad[20, 0] = float("inf"), float("nan")
+    got = fp.flarepp_linear_forward(bad, W, b)
+    keep = [i for i in range(shape[0]) if i not in (7, 20)]
+    assert torch.equal(got[keep], ref[keep])
+    assert not torch.isfinite(got[7].float()).any() and torch.isnan(got[20].float()).all()
+
+
+def _check_backward(X, W, pre, d, act, dtype, g):
+    x, w, dd = _f64(X), _f64(W), _f64(d)
+    y = None if pre is None else _f64(pre)
+    rdX, rdW, rdb = orc.linear_backward(x, w, y, dd, act)
+    dP = np.abs(dd if act == "none" else dd * orc.slope(y, act))
+    # the slope: 1e-6 of 1.13 at most beside its own rounding
+    eP = 0.0 if act == "none" else 1.2e-6 * np.abs(dd)
+    T, N = dd.shape
+    u = 2.0 ** -24
+    if "dX" in g:
+        cut = 0.0 if act == "none" else HALF[dtype]
+        err = (eP + cut * (dP + eP) + (N + 2) * u * dP) @ np.abs(w).T
+        _within("dX", g["dX"], rdX, err * (1 + HALF[dtype]) + HALF[dtype] * np.abs(rdX) + 1e-30)
+    cut = 0.0 if act == "none" else HALF[dtype] ** 2 if dtype == "bf16" else u
+    if "dW" in g:
+        _within("dW", g["dW"], rdW, np.abs(x).T @ (eP + cut * dP + (2 * T + 8) * u * (dP + eP)) + 1e-30)
+    if "dbias" in g:
+        _within("dbias", g["dbias"], rdb, (eP + (T + 8) * u * (dP + eP) + u * dP).sum(0) + 1e-30)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_backward(shape, dtype):
+    X, W, _, pre, d = _inputs(*shape, dtype, seed=4)
+    _check_backward(X, W, pre, d, "gelu", dtype, fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_GELU))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("shape", [(700, 64, 136), (2100, 37, 9)], ids=str)
+def test_backward_activations(shape, act, dtype):
+    X, W, _, pre, d = _inputs(*shape, dtype, seed=5)
+    pre = None if act == "none" else pre
+    _check_backward(X, W, pre, d, act, dtype, fp.flarepp_linear_backward(X, W, d, pre=pre, act=ACTS[act]))
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+def test_backward_against_differences(act):
+    """<dX, U> + <dW, S> + <db, s> against central differences of the float64
+    forward: their error is h^2 times a third derivative (~1e-6 here), the
+    gradients' that of fp32."""
+    T, K, N, h = 23, 17, 11, 1e-3
+    X, W, b, _, d = _inputs(T, K, N, "f32", seed=6)
+    _, pre = fp.flarepp_linear_forward(X, W, b, act=ACTS[act], keep_pre=True)
+    if act == "relu":  # away from the kink: every |pre| above the step
+        pre_ref = _f64(pre)
+        d = d * torch.from_numpy((np.abs(pre_ref) > 0.05).astype(np.float32)).cuda()
+    g = fp.flarepp_linear_backward(X, W, d, pre=pre if act != "none" else None, act=ACTS[act])
+    rng = np.random.default_rng(0)
+    U, S, s = rng.standard_normal((T, K)) * 0.1, rng.standard_normal((K, N)) * 0.1, rng.standard_normal(N) * 0.1
+    x, w, bb, dd = _f64(X), _f64(W), _f64(b), _f64(d)
+    f = lambda e: float((orc.linear_forward(x + e * U, w + e * S, bb + e * s, None, act)[0] * dd).sum())  # noqa: E731
+    want = (f(h) - f(-h)) / (2 * h)
+    got = float((_f64(g["dX"]) * U).sum() + (_f64(g["dW"]) * S).sum() + (_f64(g["dbias"]) * s).sum())
+    size = float((np.abs(_f64(g["dX"]) * U)).sum() + np.abs(_f64(g["dW"]) * S).sum())
+    assert abs(got - want) <= 1e-5 * size, (got, want, size)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_wanted_gradients_alone(dtype):
+    X, W, _, pre, d = _inputs(300, 64, 40, dtype, seed=7)
+    every = fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_SILU)
+    for k in every:
+        one = fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_SILU, **{f"want_{j}": j == k for j in every})
+        assert list(one) == [k] and torch.equal(one[k], every[k])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_leading_dimensions_and_in_place_residual(dtype):
+    X, W, b, r, _ = _inputs(60, 64, 64, dtype, seed=8)
+    ref = fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, residual=r)
+    got = fp.flarepp_linear_forward(X.view(3, 4, 5, 64), W, b, act=fp.ACT_GELU, residual=r.view(3, 4, 5, 64))
+    assert got.shape == (3, 4, 5, 64) and torch.equal(got.view(60, 64), ref)
+    assert torch.equal(fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, residual=r, out=r), ref)
+
+
+@pytest.mark.parametrize("shape", [(4000, 64, 128), (33, 1030, 12)], ids=str)
+def test_graph_replays_and_streams(shape):
+    X, W, b, r, d = _inputs(*shape, "bf16", seed=9)
+    out, pre = fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, keep_pre=True)
+    g0 = fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_GELU)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        on_side = fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_GELU)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(on_side[k], g0[k]) for k in g0)
+    o, gr = torch.empty_like(out), {k: torch.empty_like(v) for k, v in g0.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, out=o)
+        fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_GELU, out=gr)
+    for _ in range(3):
+        o.zero_()
+        for v in gr.values():
+            v.fill_(float("nan"))
+        fp.flarepp_linear_forward(r.new_ones(9, shape[1]), W)  # eager work in between
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, out) and all(torch.equal(gr[k], g0[k]) for k in g0)
