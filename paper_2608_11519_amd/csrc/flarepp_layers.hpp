@@ -38,6 +38,14 @@ constexpr int lin_step(int elem_bytes) { return 128 / elem_bytes; }
 bool lin_direct(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K);
 template <typename T> hipError_t launch_lin_gemm(const LinGemmParams&, int prod, int tile, bool direct, hipStream_t);
 
+// The same product for many rows and a strip of outputs (32, 64, 128 or 256
+// wide) whose weights fit the LDS; with act (kLinInput), L = l * act'(pre).
+constexpr size_t kLinRowsLds = 144 * 1024;
+size_t lin_rows_lds(int elem_bytes, int strip, int64_t K);
+int lin_rows_strip(int prod, int elem_bytes, int64_t Q, int64_t K);
+template <typename T>
+hipError_t launch_lin_rows(const LinGemmParams&, int prod, int strip, const void* pre, int act, hipStream_t);
+
 // out = epilogue of the sum over the splits of part
 template <typename T> hipError_t launch_lin_finish(const LinGemmParams&, hipStream_t);
 

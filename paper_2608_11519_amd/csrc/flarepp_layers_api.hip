@@ -87,7 +87,10 @@ int check_linear_shape(int dtype, int act, int64_t T, int64_t K, int64_t N) {
   return FLAREPP_OK;
 }
 
+constexpr int64_t kLinRowsFrom = 8192;  // rows from which the weights' copy into every CU pays
+
 struct LinPlan {
+  int strip;  // not 0: k_linear_rows with strips of this width
   int tile, splits;
   bool direct;
   int64_t kchunk, part_stride;
@@ -103,6 +106,9 @@ LinPlan lin_plan(int prod, int bs, int64_t P, int64_t Q, int64_t K) {
   LinPlan pl{};
   const int64_t bk = lin_step(bs), steps = cdiv(K, bk);
   const bool weight = prod == kLinWeight;
+  pl.splits = 1;
+  if (P >= kLinRowsFrom) pl.strip = lin_rows_strip(prod, bs, Q, K);
+  if (pl.strip) return pl;
   int64_t bp, bq;
   if (Q <= 32 && P > 64) { pl.tile = kTile128x32; bp = 128; bq = 32; }
   else if (P <= 32 && Q > 64) { pl.tile = kTile32x128; bp = 32; bq = 128; }
@@ -134,7 +140,8 @@ int run_linear(int act, int64_t rows, int64_t K, int64_t N, const void* X, const
   const LinPlan pl = lin_plan(kLinForward, sizeof(T), rows, N, K);
   LinGemmParams p = lin_params(pl, rows, N, K, X, W, ws);
   p.bias = bias; p.res = res; p.out = out; p.pre = pre; p.act = act;
-  HIPTRY(launch_lin_gemm<T>(p, kLinForward, pl.tile, pl.direct, s));
+  if (pl.strip) HIPTRY(launch_lin_rows<T>(p, kLinForward, pl.strip, nullptr, FLAREPP_ACT_NONE, s));
+  else HIPTRY(launch_lin_gemm<T>(p, kLinForward, pl.tile, pl.direct, s));
   if (p.part) HIPTRY(launch_lin_finish<T>(p, s));
   return api_ok();
 }
@@ -188,7 +195,12 @@ int run_linear_backward(int dtype, int act, int64_t rows, int64_t K, int64_t N, 
   if (dX) {
     LinGemmParams p = lin_params(w.dx, rows, K, N, dp, W, w.part);
     p.out = dX;
-    HIPTRY(launch_lin_gemm<T>(p, kLinInput, w.dx.tile, w.dx.direct, s));
+    if (w.dx.strip) {
+      p.l = dOut;
+      HIPTRY(launch_lin_rows<T>(p, kLinInput, w.dx.strip, pre, act, s));
+    } else {
+      HIPTRY(launch_lin_gemm<T>(p, kLinInput, w.dx.tile, w.dx.direct, s));
+    }
     if (p.part) HIPTRY(launch_lin_finish<T>(p, s));
   }
   LinSumParams sums{};

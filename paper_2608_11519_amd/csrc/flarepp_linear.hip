@@ -1,164 +1,10 @@
 // Linear layer out = res + act(X W + b) and its gradients.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
-
-#include "flarepp_device.hpp"
-#include "flarepp_layers.hpp"
+#include "flarepp_linear.hpp"
 
 namespace flarepp {
 namespace {
-
-// ---- activations ---------------------------------------------------------------
-// Phi(-|y|), the normal distribution's lower tail, by Abramowitz and Stegun
-// 7.1.26: 1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), absolute
-// error 1.5e-7 in erf.  The tail form keeps it free of cancellation for negative y.
-__device__ __forceinline__ float normal_tail(float y, float& gauss) {
-  const float x = __builtin_fabsf(y) * 0.70710678f;
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
-  gauss = __builtin_amdgcn_exp2f(y * y * -0.72134752f);  // exp(-y^2 / 2)
-  float q = 1.061405429f;
-  q = __builtin_fmaf(q, t, -1.453152027f);
-  q = __builtin_fmaf(q, t, 1.421413741f);
-  q = __builtin_fmaf(q, t, -0.284496736f);
-  q = __builtin_fmaf(q, t, 0.254829592f);
-  return 0.5f * q * t * gauss;
-}
-__device__ __forceinline__ float sigmoid(float y) {
-  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y * -1.44269504f));
-}
-__device__ __forceinline__ float activate(float y, int act) {
-  if (act == kActRelu) return y < 0.f ? 0.f : y;  // a NaN stays
-  if (act == kActGelu) {
-    float gauss;
-    const float tail = normal_tail(y, gauss);
-    return y * (y < 0.f ? tail : 1.f - tail);
-  }
-  if (act == kActSilu) return y * sigmoid(y);
-  return y;
-}
-__device__ __forceinline__ float slope(float y, int act) {
-  if (act == kActRelu) return y > 0.f ? 1.f : 0.f;
-  if (act == kActGelu) {
-    float gauss;
-    const float tail = normal_tail(y, gauss);
-    return __builtin_fmaf(y * 0.39894228f, gauss, y < 0.f ? tail : 1.f - tail);
-  }
-  if (act == kActSilu) {
-    const float s = sigmoid(y);
-    return s * __builtin_fmaf(y, 1.f - s, 1.f);
-  }
-  return 1.f;
-}
-
-// ---- operand tiles in LDS ----------------------------------------------------------
-// A step holds 128 bytes of the reduction of every row.  k-contiguous operands
-// lie as [ROWS][128 bytes] with a row's eight 16-byte chunks permuted by the row
-// (reads of one chunk of 8 rows fall in different banks); the others as
-// [k][ROWS] with pairs of chunks permuted by k, for the transposing reads.
-template <typename T, bool TR, int ROWS> struct Tile {
-  static constexpr int EPC = 16 / (int)sizeof(T), BK = 128 / (int)sizeof(T);
-  static constexpr int CPR = TR ? ROWS / EPC : 8;  // chunks of a stored row
-  static constexpr int BYTES = ROWS * 128, CHUNKS = ROWS * 8;
-  // the source chunk that LDS slot s of stored row `row` holds (an involution)
-  static __device__ __forceinline__ int swap(int row, int s) {
-    if constexpr (!TR) return s ^ (row & 7);
-    else if constexpr (sizeof(T) == 4) return s;
-    else return s ^ (ROWS >= 128 ? 2 * (row & 7) : ROWS == 64 ? 2 * ((row >> 1) & 3) : 2 * ((row >> 2) & 1));
-  }
-  // rows 32 blk .. + 31, reduction elements 16 ks .. + 15: lane (c, g) holds
-  // row c, elements 8 g .. + 7
-  static __device__ __forceinline__ typename Frag<T>::type frag(const char* buf, int blk, int ks) {
-    const int lane = lane_id(), g = lane >> 5, c = lane & 31;
-    if constexpr (!TR && sizeof(T) == 2) {
-      const int row = 32 * blk + c;
-      return load_frag(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 2 * ks + g) * 16));
-    } else if constexpr (!TR) {
-      const int row = 32 * blk + c;
-      return join<T>(load_half(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 4 * ks + 2 * g) * 16)),
-                     load_half(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 4 * ks + 2 * g + 1) * 16)));
-    } else if constexpr (sizeof(T) == 2) {
-      const int i16 = lane & 15, k = 16 * ks + 8 * g + (i16 >> 2);
-      const int s = 4 * blk + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
-      return lds_tr_frag(buf + k * ROWS * 2 + swap(k, s) * 16 + 8 * (i16 & 1),
-                         buf + (k + 4) * ROWS * 2 + swap(k + 4, s) * 16 + 8 * (i16 & 1));
-    } else {
-      const T* p = reinterpret_cast<const T*>(buf) + (16 * ks + 8 * g) * ROWS + 32 * blk + c;
-      typename Frag<T>::type f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = p[j * ROWS];
-      return f;
-    }
-  }
-};
-
-// One 16-byte chunk of an operand with `rows` rows and reduction length kend,
-// zeros outside; by elements where rows of the array are not whole chunks.
-template <typename T, bool TR>
-__device__ __forceinline__ f32x4 guarded_chunk(const T* src, int64_t ld, int64_t rows, int64_t kend, int64_t row, int64_t k,
-                                               bool whole) {
-  constexpr int EPC = 16 / (int)sizeof(T);
-  // stored row and column, and their ends
-  const int64_t sr = TR ? k : row, sc = TR ? row : k, re = TR ? kend : rows, ce = TR ? rows : kend;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (sr >= re) return v;
-  const T* s = src + sr * ld + sc;
-  if (whole) {
-    if (sc < ce) v = *reinterpret_cast<const f32x4*>(s);
-    return v;
-  }
-  T e[EPC];
-#pragma unroll
-  for (int j = 0; j < EPC; ++j) e[j] = sc + j < ce ? s[j] : from_f32<T>(0.f);
-  __builtin_memcpy(&v, e, 16);
-  return v;
-}
-
-// ---- epilogue ---------------------------------------------------------------------
-// Four consecutive outputs q .. q + 3 of row p: bias, activation, residual;
-// the pre-activation's values stay in y.
-template <typename T>
-__device__ __forceinline__ void finish(float (&y)[4], float (&o)[4], const LinGemmParams& p, int64_t row, int64_t q, bool whole) {
-  const T* bias = static_cast<const T*>(p.bias);
-  const T* res = static_cast<const T*>(p.res);
-  float b[4] = {0.f, 0.f, 0.f, 0.f}, r[4] = {0.f, 0.f, 0.f, 0.f};
-  if (whole) {
-    if (bias) {
-      const auto v = load_half(bias + q);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) b[e] = to_f32(v[e]);
-    }
-    if (res) {
-      const auto v = load_half(res + row * p.Q + q);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) r[e] = to_f32(v[e]);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (q + e < p.Q) {
-        if (bias) b[e] = to_f32(bias[q + e]);
-        if (res) r[e] = to_f32(res[row * p.Q + q + e]);
-      }
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (bias) y[e] += b[e];
-    o[e] = activate(y[e], p.act);
-    if (res) o[e] += r[e];
-  }
-}
-template <typename T>
-__device__ __forceinline__ void store_part(T* out, int64_t Q, int64_t row, int64_t q, const float (&v)[4], bool whole) {
-  if (whole) {
-    store4(out + row * Q + q, v[0], v[1], v[2], v[3]);
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (q + e < Q) out[row * Q + q + e] = from_f32<T>(v[e]);
-}
 
 // ---- the product -------------------------------------------------------------------
 template <typename T, int PROD, bool LO, int BP, int BQ, int WP, int WQ, bool DIRECT, int NBUF>
@@ -309,65 +155,43 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
     }
   }
 
-  // lane (c, g) holds row p = c, outputs 8 u + 4 g .. + 3 of every block
-  const bool whole = p.Q % (p.part ? 4 : EPC) == 0;
 #pragma unroll
   for (int j = 0; j < NP; ++j) {
     const int64_t row = p0 + 32 * (wp * NP + j) + c;
-    const bool in = row < p.P;
-    const int64_t rr = min(row, p.P - 1);
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       const int64_t qb = q0 + 32 * (wq * NQ + i);
       if (qb >= p.Q) continue;
+      if (!p.part) {
+        if (p.Q % EPC == 0 && qb + 32 <= p.Q) {
+          const int64_t at = min(row, p.P - 1) * p.Q + qb;
+          auto bias = [&](f32x16& y) __attribute__((always_inline)) {
+            if (!p.bias) return;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float y[2][4], o[2][4];
+            for (int u = 0; u < 4; ++u) {
+              const auto v = load_half(static_cast<const T*>(p.bias) + qb + 8 * u + 4 * g);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[h][e] = acc[i][j][8 * u + 4 * h + e];
-        if (p.part) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int64_t q = qb + 16 * u + 8 * h + 4 * g;
-            if (in && q < p.Q) store_part(p.part + z * p.part_stride, p.Q, row, q, y[h], whole);
-          }
-          continue;
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int64_t q = qb + 16 * u + 8 * h + 4 * g;
-          if (q < p.Q) finish<T>(y[h], o[h], p, rr, q, whole);
-          else o[h][0] = o[h][1] = o[h][2] = o[h][3] = 0.f;
-        }
-        if (whole && sizeof(T) == 2) {
-          // runs of 8 outputs per lane
-          const int64_t q = qb + 16 * u + 8 * g;
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = o[e / 4][e % 4];
-          bf16x8 w;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = (__bf16)v[e];
-          w = runs_of_8(w);
-          if (in && q < p.Q) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.out) + row * p.Q + q) = w;
-          if (p.pre) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = (__bf16)y[e / 4][e % 4];
-            w = runs_of_8(w);
-            if (in && q < p.Q) *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p.pre) + row * p.Q + q) = w;
-          }
-        } else {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int64_t q = qb + 16 * u + 8 * h + 4 * g;
-            if (in && q < p.Q) {
-              store_part(static_cast<T*>(p.out), p.Q, row, q, o[h], whole);
-              if (p.pre) store_part(static_cast<T*>(p.pre), p.Q, row, q, y[h], whole);
+              for (int e = 0; e < 4; ++e) y[4 * u + e] += to_f32(v[e]);
             }
-          }
+          };
+          with_act(p.act, [&](auto act) __attribute__((always_inline)) {
+            epilogue_whole<T, decltype(act)::value>(acc[i][j], p.res ? static_cast<const T*>(p.res) + at : nullptr,
+                                                    static_cast<T*>(p.out) + at, p.pre ? static_cast<T*>(p.pre) + at : nullptr,
+                                                    row < p.P, bias);
+          });
+        } else {
+          epilogue_parts<T>(acc[i][j], p, row, qb);
         }
+        continue;
+      }
+      const bool whole = p.Q % 4 == 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t q = qb + 8 * u + 4 * g;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * u + e];
+        if (row < p.P && q < p.Q) store_part(p.part + z * p.part_stride, p.Q, row, q, v, whole);
       }
     }
   }
@@ -393,7 +217,7 @@ __global__ __launch_bounds__(256) void k_linear_finish(LinGemmParams p) {
         if (q + e < p.Q) y[e] += s[e];
     }
   }
-  finish<T>(y, o, p, row, q, whole);
+  finish4<T>(y, o, p, row, q, whole);
   store_part(static_cast<T*>(p.out), p.Q, row, q, o, whole);
   if (p.pre) store_part(static_cast<T*>(p.pre), p.Q, row, q, y, whole);
 }
@@ -401,7 +225,7 @@ __global__ __launch_bounds__(256) void k_linear_finish(LinGemmParams p) {
 // ---- dP = dOut * act'(pre) and its column sums --------------------------------------------
 // A workgroup takes a chunk of rows and a strip of columns: VEC (16 bytes) or
 // one column per lane, CL lanes across, 256 / CL rows at a time.
-template <typename T, int VEC>
+template <typename T, int VEC, int ACT>
 __global__ __launch_bounds__(256) void k_linear_slope(LinSlopeParams p, int cl_log2) {
   __shared__ float sums[256 * VEC];
   const int cl = 1 << cl_log2, lc = threadIdx.x & (cl - 1), lr = threadIdx.x >> cl_log2, rl = 256 >> cl_log2;
@@ -417,11 +241,11 @@ __global__ __launch_bounds__(256) void k_linear_slope(LinSlopeParams p, int cl_l
       const int64_t at = r * p.N + col;
       T dv[VEC], av[VEC], hi[VEC], lo[VEC];
       __builtin_memcpy(dv, __builtin_assume_aligned(d + at, VEC * sizeof(T)), VEC * sizeof(T));
-      if (p.act != kActNone) __builtin_memcpy(av, __builtin_assume_aligned(a + at, VEC * sizeof(T)), VEC * sizeof(T));
+      if (ACT != kActNone) __builtin_memcpy(av, __builtin_assume_aligned(a + at, VEC * sizeof(T)), VEC * sizeof(T));
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         float v = to_f32(dv[e]);
-        if (p.act != kActNone) v *= slope(to_f32(av[e]), p.act);
+        if (ACT != kActNone) v *= slope<ACT>(to_f32(av[e]));
         s[e] += v;
         hi[e] = from_f32<T>(v);
         lo[e] = from_f32<T>(v - to_f32(hi[e]));
@@ -528,8 +352,15 @@ hipError_t launch_lin_slope(const LinSlopeParams& p, hipStream_t s) {
   int cl = 0;
   while ((1 << cl) < (vec == 1 ? 256 : 32) && (int64_t)vec << cl < p.N) ++cl;
   const dim3 grid((unsigned)p.nchunks, (unsigned)((p.N + ((int64_t)vec << cl) - 1) / ((int64_t)vec << cl)));
-  if (vec == 1) k_linear_slope<T, 1><<<grid, 256, 0, s>>>(p, cl);
-  else k_linear_slope<T, V><<<grid, 256, 0, s>>>(p, cl);
+  auto go = [&](auto act) {
+    constexpr int A = decltype(act)::value;
+    if (vec == 1) k_linear_slope<T, 1, A><<<grid, 256, 0, s>>>(p, cl);
+    else k_linear_slope<T, V, A><<<grid, 256, 0, s>>>(p, cl);
+  };
+  if (p.act == kActGelu) go(ActC<kActGelu>{});
+  else if (p.act == kActSilu) go(ActC<kActSilu>{});
+  else if (p.act == kActRelu) go(ActC<kActRelu>{});
+  else go(ActC<kActNone>{});
   return hipGetLastError();
 }
 template hipError_t launch_lin_slope<float>(const LinSlopeParams&, hipStream_t);

@@ -1,0 +1,226 @@
+// Shared by the kernels of the linear layer: activations, operand tiles in LDS,
+// the epilogue.
+#pragma once
+
+#include <algorithm>
+
+#include "flarepp_device.hpp"
+#include "flarepp_layers.hpp"
+
+namespace flarepp {
+namespace {
+
+// ---- activations ---------------------------------------------------------------
+// Phi(-|y|), the normal distribution's lower tail, by Abramowitz and Stegun
+// 7.1.26: 1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), absolute
+// error 1.5e-7 in erf.  The tail form keeps it free of cancellation for negative y.
+__device__ __forceinline__ float normal_tail(float y, float& gauss) {
+  const float x = __builtin_fabsf(y) * 0.70710678f;
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
+  gauss = __builtin_amdgcn_exp2f(y * y * -0.72134752f);  // exp(-y^2 / 2)
+  float q = 1.061405429f;
+  q = __builtin_fmaf(q, t, -1.453152027f);
+  q = __builtin_fmaf(q, t, 1.421413741f);
+  q = __builtin_fmaf(q, t, -0.284496736f);
+  q = __builtin_fmaf(q, t, 0.254829592f);
+  return 0.5f * q * t * gauss;
+}
+__device__ __forceinline__ float sigmoid(float y) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y * -1.44269504f));
+}
+template <int ACT> __device__ __forceinline__ float activate(float y) {
+  if constexpr (ACT == kActRelu) return y < 0.f ? 0.f : y;  // a NaN stays
+  if constexpr (ACT == kActGelu) {
+    float gauss;
+    const float tail = normal_tail(y, gauss);
+    return y * (y < 0.f ? tail : 1.f - tail);
+  }
+  if constexpr (ACT == kActSilu) return y * sigmoid(y);
+  return y;
+}
+template <int ACT> __device__ __forceinline__ float slope(float y) {
+  if constexpr (ACT == kActRelu) return y > 0.f ? 1.f : 0.f;
+  if constexpr (ACT == kActGelu) {
+    float gauss;
+    const float tail = normal_tail(y, gauss);
+    return __builtin_fmaf(y * 0.39894228f, gauss, y < 0.f ? tail : 1.f - tail);
+  }
+  if constexpr (ACT == kActSilu) {
+    const float s = sigmoid(y);
+    return s * __builtin_fmaf(y, 1.f - s, 1.f);
+  }
+  return 1.f;
+}
+// f with the activation as a constant (one uniform branch for a whole block)
+template <int V> struct ActC { static constexpr int value = V; };
+template <typename Fn> __device__ __forceinline__ void with_act(int act, Fn f) {
+  if (act == kActGelu) f(ActC<kActGelu>{});
+  else if (act == kActSilu) f(ActC<kActSilu>{});
+  else if (act == kActRelu) f(ActC<kActRelu>{});
+  else f(ActC<kActNone>{});
+}
+
+// ---- operand tiles in LDS ----------------------------------------------------------
+// A step holds 128 bytes of the reduction of every row.  k-contiguous operands
+// lie as [ROWS][128 bytes] with a row's eight 16-byte chunks permuted by the
+// row, the others as [k][ROWS] with groups of four chunks permuted by k for the
+// transposing reads: the 256 bytes of a read's turn (one chunk of 16 rows; 64
+// bytes of four k) fall in different banks.
+template <typename T, bool TR, int ROWS> struct Tile {
+  static constexpr int EPC = 16 / (int)sizeof(T), BK = 128 / (int)sizeof(T);
+  static constexpr int CPR = TR ? ROWS / EPC : 8;  // chunks of a stored row
+  static constexpr int BYTES = ROWS * 128, CHUNKS = ROWS * 8;
+  // the source chunk that LDS slot s of stored row `row` holds (an involution)
+  static __device__ __forceinline__ int swap(int row, int s) {
+    if constexpr (!TR) return s ^ (row >> 1 & 7);
+    else if constexpr (sizeof(T) == 4) return s;
+    else return s ^ (ROWS >= 128 ? 4 * (row & 3) : ROWS == 64 ? 4 * (row >> 1 & 1) : 0);
+  }
+  // rows 32 blk .. + 31, reduction elements 16 ks .. + 15: lane (c, g) holds
+  // row c, elements 8 g .. + 7
+  static __device__ __forceinline__ typename Frag<T>::type frag(const char* buf, int blk, int ks) {
+    const int lane = lane_id(), g = lane >> 5, c = lane & 31;
+    if constexpr (!TR && sizeof(T) == 2) {
+      const int row = 32 * blk + c;
+      return load_frag(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 2 * ks + g) * 16));
+    } else if constexpr (!TR) {
+      const int row = 32 * blk + c;
+      return join<T>(load_half(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 4 * ks + 2 * g) * 16)),
+                     load_half(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 4 * ks + 2 * g + 1) * 16)));
+    } else if constexpr (sizeof(T) == 2) {
+      const int i16 = lane & 15, k = 16 * ks + 8 * g + (i16 >> 2);
+      const int s = 4 * blk + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+      return lds_tr_frag(buf + k * ROWS * 2 + swap(k, s) * 16 + 8 * (i16 & 1),
+                         buf + (k + 4) * ROWS * 2 + swap(k + 4, s) * 16 + 8 * (i16 & 1));
+    } else {
+      const T* p = reinterpret_cast<const T*>(buf) + (16 * ks + 8 * g) * ROWS + 32 * blk + c;
+      typename Frag<T>::type f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = p[j * ROWS];
+      return f;
+    }
+  }
+};
+
+// One 16-byte chunk of an operand with `rows` rows and reduction length kend,
+// zeros outside; by elements where rows of the array are not whole chunks.
+template <typename T, bool TR>
+__device__ __forceinline__ f32x4 guarded_chunk(const T* src, int64_t ld, int64_t rows, int64_t kend, int64_t row, int64_t k,
+                                               bool whole) {
+  constexpr int EPC = 16 / (int)sizeof(T);
+  // stored row and column, and their ends
+  const int64_t sr = TR ? k : row, sc = TR ? row : k, re = TR ? kend : rows, ce = TR ? rows : kend;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (sr >= re) return v;
+  const T* s = src + sr * ld + sc;
+  if (whole) {
+    if (sc < ce) v = *reinterpret_cast<const f32x4*>(s);
+    return v;
+  }
+  T e[EPC];
+#pragma unroll
+  for (int j = 0; j < EPC; ++j) e[j] = sc + j < ce ? s[j] : from_f32<T>(0.f);
+  __builtin_memcpy(&v, e, 16);
+  return v;
+}
+
+// ---- epilogue ---------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ void store_part(T* out, int64_t Q, int64_t row, int64_t q, const float (&v)[4], bool whole) {
+  if (whole) {
+    store4(out + row * Q + q, v[0], v[1], v[2], v[3]);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (q + e < Q) out[row * Q + q + e] = from_f32<T>(v[e]);
+}
+// Four consecutive values from q on, zeros past the end of the row
+template <typename T>
+__device__ __forceinline__ void read_part(const T* src, int64_t at, int64_t q, int64_t Q, bool whole, float (&v)[4]) {
+  if (whole) {
+    const auto x = load_half(src + at + q);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = to_f32(x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = q + e < Q ? to_f32(src[at + q + e]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void finish4(float (&y)[4], float (&o)[4], const LinGemmParams& p, int64_t row, int64_t q, bool whole) {
+  float b[4], r[4];
+  if (p.bias) {
+    read_part(static_cast<const T*>(p.bias), 0, q, p.Q, whole, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] += b[e];
+  }
+  with_act(p.act, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = activate<decltype(act)::value>(y[e]);
+  });
+  if (p.res) {
+    read_part(static_cast<const T*>(p.res), row * p.Q, q, p.Q, whole, r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += r[e];
+  }
+}
+
+// One 32 x 32 block of C inside the row (Q % EPC == 0): lane (c, g) holds row c,
+// outputs 8 u + 4 g .. + 3 of the block in y[4 u ..].  res, out and pre point to
+// the row's first output of the block (or are null); bias(u) gives the four
+// biases of run u.  Stores of 16 bytes per lane.
+template <typename T, int ACT, typename Bias>
+__device__ __forceinline__ void epilogue_whole(f32x16 y, const T* res, T* out, T* pre, bool in, Bias bias) {
+  const int g = lane_id() >> 5;
+  typename Frag<T>::half r[4];
+  if (res) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) r[u] = load_half(res + 8 * u + 4 * g);
+  }
+  bias(y);
+  auto put = [&](T* d, const f32x16& v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (sizeof(T) == 2) {
+        bf16x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = (__bf16)v[8 * u + e];
+        w = runs_of_8(w);
+        if (in) *reinterpret_cast<bf16x8*>(d + 16 * u + 8 * g) = w;
+      } else if (in) {
+        store4(d + 16 * u + 4 * g, v[8 * u], v[8 * u + 1], v[8 * u + 2], v[8 * u + 3]);
+        store4(d + 16 * u + 8 + 4 * g, v[8 * u + 4], v[8 * u + 5], v[8 * u + 6], v[8 * u + 7]);
+      }
+    }
+  };
+  if (pre) put(pre, y);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) y[e] = activate<ACT>(y[e]);
+  if (res) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) y[e] += to_f32(r[e / 4][e % 4]);
+  }
+  put(out, y);
+}
+// the same for rows of any width and blocks that pass the row's end
+template <typename T>
+__device__ __forceinline__ void epilogue_parts(const f32x16& y, const LinGemmParams& p, int64_t row, int64_t qb) {
+  const int g = lane_id() >> 5;
+  const bool whole = p.Q % 4 == 0;
+  if (row >= p.P) return;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int64_t q = qb + 8 * u + 4 * g;
+    if (q >= p.Q) continue;
+    float v[4], o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = y[4 * u + e];
+    finish4<T>(v, o, p, row, q, whole);
+    store_part(static_cast<T*>(p.out), p.Q, row, q, o, whole);
+    if (p.pre) store_part(static_cast<T*>(p.pre), p.Q, row, q, v, whole);
+  }
+}
+
+}  // namespace
+}  // namespace flarepp

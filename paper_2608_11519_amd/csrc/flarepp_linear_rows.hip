@@ -1,0 +1,215 @@
+// Linear-layer products over many rows with the weights resident in LDS.
+#include <hip/hip_runtime.h>
+
+#include "flarepp_linear.hpp"
+
+namespace flarepp {
+namespace {
+
+// C[P][Q] = L[P][K] R[K][Q] for a strip of NB outputs whose weights fit the
+// LDS: persistent workgroups of eight waves, each wave walking tiles of 32 rows
+// on its own.  Rows come straight from memory as MFMA fragments, a segment of SEG
+// 16-element steps ahead, so every element of L passes a CU once and no barrier
+// follows the weights' copy.  SLOPE: L = l * act'(pre), formed in registers.
+// STEPS: K is whole steps of 16 (else rows are read by single elements).
+// WHOLE: Q is whole blocks of 32.
+template <typename T, bool RT, int NB, bool SLOPE, bool STEPS, bool WHOLE>
+__global__ __launch_bounds__(512) void k_linear_rows(LinGemmParams p, const void* slope_pre, int slope_act) {
+  using F = typename Frag<T>::type;
+  using R = Tile<T, RT, NB>;
+  constexpr int EPC = R::EPC, BK = R::BK, NQ = NB / 32, KPB = BK / 16;  // steps of a buffer of BK
+  constexpr int SEG = !STEPS ? 1 : SLOPE || sizeof(T) == 4 || NB == 256 ? 4 : 8;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int lane = lane_id(), wave = wave_id(), g = lane >> 5, c = lane & 31;
+  const int64_t q0 = (int64_t)blockIdx.y * NB;
+  const int K = (int)p.K, KS = (K + 15) / 16, nbuf = (KS + KPB - 1) / KPB;
+
+  // the strip's weights, zeros past the end of the reduction, and its biases
+  float* lbias = reinterpret_cast<float*>(smem + nbuf * R::BYTES);
+  if (WHOLE && p.bias && threadIdx.x < NB)
+    lbias[threadIdx.x] = q0 + threadIdx.x < p.Q ? to_f32(static_cast<const T*>(p.bias)[q0 + threadIdx.x]) : 0.f;
+  {
+    const T* w = static_cast<const T*>(p.r);
+    const int64_t ld = RT ? p.Q : p.K;
+    const bool whole = ld % EPC == 0;
+    const int chunks = nbuf * R::CHUNKS;
+    for (int e0 = threadIdx.x; e0 < chunks; e0 += 512 * 8) {
+      f32x4 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int e = e0 + u * 512;
+        if (e >= chunks) break;
+        // RT: stored rows run through all buffers; else a buffer holds BK elements of every row
+        const int b = e / R::CHUNKS, ee = e % R::CHUNKS, row = ee / R::CPR, ch = R::swap(row, ee % R::CPR);
+        v[u] = RT ? guarded_chunk<T, true>(w, ld, p.Q, K, q0 + ch * EPC, b * BK + row, whole)
+                  : guarded_chunk<T, false>(w, ld, p.Q, K, q0 + row, b * BK + ch * EPC, whole);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int e = e0 + u * 512;
+        if (e >= chunks) break;
+        reinterpret_cast<f32x4*>(smem)[e] = v[u];
+      }
+    }
+  }
+  const int64_t tiles = (p.P + 31) / 32, stride = (int64_t)gridDim.x * 8;
+  int64_t tile = (int64_t)blockIdx.x * 8 + wave;
+  const int nseg = (KS + SEG - 1) / SEG;
+
+  struct Rows {
+    F x[SEG];
+    F y[SLOPE ? SEG : 1];
+  };
+  auto load = [&](Rows& r, int64_t t, int seg) __attribute__((always_inline)) {
+    const int64_t at = min(t * 32 + c, p.P - 1) * K;
+    const T* l = static_cast<const T*>(p.l) + at;
+    const T* y = SLOPE ? static_cast<const T*>(slope_pre) + at : nullptr;
+#pragma unroll
+    for (int j = 0; j < SEG; ++j) {
+      const int k = (seg * SEG + j) * 16 + 8 * g;
+      if constexpr (STEPS) {
+        const int kc = min(k, K - 16 + 8 * g);  // steps past the end are not used
+        r.x[j] = load_frag(l + kc);
+        if constexpr (SLOPE) r.y[j] = load_frag(y + kc);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int kc = min(k + e, K - 1);
+          const T v = l[kc];
+          r.x[j][e] = k + e < K ? v : from_f32<T>(0.f);
+          if constexpr (SLOPE) r.y[j][e] = y[kc];
+        }
+      }
+    }
+  };
+
+  f32x16 acc[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+
+  Rows now, next;
+  if (tile < tiles) load(now, tile, 0);
+  __syncthreads();
+  int seg = 0;
+  while (tile < tiles) {
+    // the next segment's loads, this one's products, and a tile's end
+    const bool last = seg == nseg - 1;
+    const int64_t ntile = last ? tile + stride : tile;
+    const int nxt = last ? 0 : seg + 1;
+    if (ntile < tiles) load(next, ntile, nxt);
+    auto step = [&](int j) __attribute__((always_inline)) {
+      const int ks = seg * SEG + j;
+      F x = now.x[j];
+      if constexpr (SLOPE) {
+        with_act(slope_act, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float v = to_f32(x[e]) * slope<decltype(act)::value>(to_f32(now.y[j][e]));
+            x[e] = from_f32<T>(STEPS || ks * 16 + 8 * g + e < K ? v : 0.f);
+          }
+        });
+      }
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+        mma(acc[i], RT ? R::frag(smem, i, ks) : R::frag(smem + ks / KPB * R::BYTES, i, ks % KPB), x);
+    };
+#pragma unroll
+    for (int j = 0; j < SEG; ++j)
+      if (seg * SEG + j < KS) step(j);  // uniform
+    if (last) {
+      const int64_t row = tile * 32 + c;
+      const int64_t at = min(row, p.P - 1) * p.Q + q0;
+      const T* res = p.res ? static_cast<const T*>(p.res) + at : nullptr;
+      T* out = static_cast<T*>(p.out) + at;
+      T* pre = p.pre ? static_cast<T*>(p.pre) + at : nullptr;
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        if (q0 + 32 * i < p.Q) {
+          if constexpr (WHOLE) {
+            auto bias = [&](f32x16& y) __attribute__((always_inline)) {
+              if (!p.bias) return;
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(lbias + 32 * i + 8 * u + 4 * g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[4 * u + e] += v[e];
+              }
+            };
+            with_act(p.act, [&](auto act) __attribute__((always_inline)) {
+              epilogue_whole<T, decltype(act)::value>(acc[i], res ? res + 32 * i : nullptr, out + 32 * i,
+                                                      pre ? pre + 32 * i : nullptr, row < p.P, bias);
+            });
+          } else {
+            epilogue_parts<T>(acc[i], p, row, q0 + 32 * i);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+      }
+    }
+    now = next;
+    tile = ntile;
+    seg = nxt;
+  }
+}
+
+template <typename T, bool RT, int NB, bool SLOPE, bool STEPS, bool WHOLE>
+hipError_t launch_strip(const LinGemmParams& p, const void* pre, int act, hipStream_t s) {
+  const int64_t tiles = (p.P + 31) / 32, strips = (p.Q + NB - 1) / NB;
+  const size_t lds = lin_rows_lds(sizeof(T), NB, p.K);
+  const int64_t groups = std::min<int64_t>((tiles + 7) / 8, std::max<int64_t>(1, 256 / strips));
+  auto* kernel = k_linear_rows<T, RT, NB, SLOPE, STEPS, WHOLE>;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  if (e != hipSuccess) return e;
+  kernel<<<dim3((unsigned)groups, (unsigned)strips), 512, lds, s>>>(p, pre, act);
+  return hipGetLastError();
+}
+
+template <typename T, bool RT, bool SLOPE>
+hipError_t launch_form(const LinGemmParams& p, int strip, const void* pre, int act, hipStream_t s) {
+  const bool whole = p.Q % 32 == 0, steps = p.K % 16 == 0;
+  if constexpr (RT) {
+    if (!whole && strip == 32) return launch_strip<T, RT, 32, SLOPE, true, false>(p, pre, act, s);
+    if (!whole) return launch_strip<T, RT, 64, SLOPE, true, false>(p, pre, act, s);
+  }
+#define FORM(NB) return steps ? launch_strip<T, RT, NB, SLOPE, true, true>(p, pre, act, s) : launch_strip<T, RT, NB, SLOPE, false, true>(p, pre, act, s)
+  if constexpr (sizeof(T) == 2) {
+    if (strip == 256) FORM(256);
+    if (strip == 128) FORM(128);
+  }
+  if (strip == 64) FORM(64);
+  FORM(32);
+#undef FORM
+}
+
+}  // namespace
+
+size_t lin_rows_lds(int elem_bytes, int strip, int64_t K) {
+  const int64_t bk = lin_step(elem_bytes);
+  return (size_t)((K + bk - 1) / bk) * strip * 128 + strip * sizeof(float);
+}
+
+// The strip for a product, or 0 where another kernel has to do: rows of L that
+// are whole steps, or short; outputs that are whole blocks, or (forward) few;
+// weights that fit; and L read at most twice.
+int lin_rows_strip(int prod, int elem_bytes, int64_t Q, int64_t K) {
+  const bool whole = Q % 32 == 0, steps = K % 16 == 0;
+  if (prod == kLinWeight || K > 4096 || (!steps && (K > 32 || !whole)) || (!whole && (prod != kLinForward || Q > 64))) return 0;
+  const int widest = elem_bytes == 2 ? 256 : 64;
+  int strip = 32;
+  while (strip < widest && strip < Q) strip *= 2;
+  while (strip > 32 && lin_rows_lds(elem_bytes, strip, K) > kLinRowsLds) strip /= 2;
+  return lin_rows_lds(elem_bytes, strip, K) <= kLinRowsLds && (Q + strip - 1) / strip <= 2 ? strip : 0;
+}
+
+template <typename T>
+hipError_t launch_lin_rows(const LinGemmParams& p, int prod, int strip, const void* pre, int act, hipStream_t s) {
+  if (prod == kLinForward) return launch_form<T, true, false>(p, strip, nullptr, kActNone, s);
+  return act == kActNone ? launch_form<T, false, false>(p, strip, nullptr, act, s) : launch_form<T, false, true>(p, strip, pre, act, s);
+}
+template hipError_t launch_lin_rows<float>(const LinGemmParams&, int, int, const void*, int, hipStream_t);
+template hipError_t launch_lin_rows<__bf16>(const LinGemmParams&, int, int, const void*, int, hipStream_t);
+
+}  // namespace flarepp
