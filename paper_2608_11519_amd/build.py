@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libflarepp.so")
 SOURCES = ["flarepp_kernels.hip", "flarepp_fused.hip", "flarepp_backward.hip",
            "flarepp_attn_bwd.hip", "flarepp_grad_gemm.hip", "flarepp_api.hip",
-           "flarepp_linear.hip", "flarepp_linear_rows.hip", "flarepp_embedding.hip", "flarepp_adamw.hip", "flarepp_layers_api.hip"]
+           "flarepp_linear.hip", "flarepp_linear_rows.hip", "flarepp_linear_bwd.hip",
+           "flarepp_embedding.hip", "flarepp_adamw.hip", "flarepp_layers_api.hip"]
 ARCH = "gfx950"
 
 

@@ -20,7 +20,7 @@ constexpr bool lin_l_t(int prod) { return prod == kLinWeight; }
 constexpr bool lin_r_t(int prod) { return prod != kLinInput; }
 
 // Output tiles (P x Q) of a workgroup
-enum LinTile { kTile128 = 0, kTile64 = 1, kTile128x32 = 2, kTile32x128 = 3 };
+enum LinTile { kTile128 = 0, kTile64 = 1, kTile128x32 = 2, kTile32x128 = 3, kTile256 = 4 };
 
 struct LinGemmParams {
   const void* l; const void* r;
@@ -39,12 +39,12 @@ bool lin_direct(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K);
 template <typename T> hipError_t launch_lin_gemm(const LinGemmParams&, int prod, int tile, bool direct, hipStream_t);
 
 // The same product for many rows and a strip of outputs (32, 64, 128 or 256
-// wide) whose weights fit the LDS; with act (kLinInput), L = l * act'(pre).
+// wide) whose weights fit the LDS.
 constexpr size_t kLinRowsLds = 144 * 1024;
 size_t lin_rows_lds(int elem_bytes, int strip, int64_t K);
 int lin_rows_strip(int prod, int elem_bytes, int64_t Q, int64_t K);
 template <typename T>
-hipError_t launch_lin_rows(const LinGemmParams&, int prod, int strip, const void* pre, int act, hipStream_t);
+hipError_t launch_lin_rows(const LinGemmParams&, int prod, int strip, hipStream_t);
 
 // out = epilogue of the sum over the splits of part
 template <typename T> hipError_t launch_lin_finish(const LinGemmParams&, hipStream_t);
@@ -59,6 +59,19 @@ struct LinSlopeParams {
   int nchunks; int64_t chunk;
 };
 template <typename T> hipError_t launch_lin_slope(const LinSlopeParams&, hipStream_t);
+
+// bf16: dP, dbias, dW and (fused) dX in one pass over the tokens
+struct LinBwdParams {
+  const void *x, *w, *pre, *dout;
+  void* dx;                 // fused: or null
+  void* hi;                 // not fused, act: dP rounded to bf16, or null
+  float* part; int64_t part_stride;      // [nchunks] dW of each chunk, or null
+  float* bias_part; int64_t bias_ld;     // [nchunks][bias_ld], or null
+  int64_t T, K, N, chunk;
+  int nchunks, act;
+};
+bool lin_bwd_tile(int64_t K, int64_t N, int& kt, int& nt, bool& fused);
+hipError_t launch_lin_bwd(const LinBwdParams&, int kt, int nt, bool fused, hipStream_t);
 
 // out[i] = sum_s part[s * stride + i], i < n: two independent jobs in a launch
 struct LinSumJob { const float* part; int64_t stride, n; int splits; float* out; };

@@ -114,7 +114,11 @@ LinPlan lin_plan(int prod, int bs, int64_t P, int64_t Q, int64_t K) {
   else if (P <= 32 && Q > 64) { pl.tile = kTile32x128; bp = 32; bq = 128; }
   else if (P > 64 && Q > 64 && (weight || cdiv(P, 128) * cdiv(Q, 128) >= 256)) { pl.tile = kTile128; bp = bq = 128; }
   else { pl.tile = kTile64; bp = bq = 64; }
-  pl.direct = (pl.tile == kTile128 || pl.tile == kTile64) && lin_direct(prod, bs, P, Q, K);
+  if (pl.tile == kTile128 && !weight && bs == 2 && lin_direct(prod, bs, P, Q, K)) {
+    const int64_t t = cdiv(P, 256) * cdiv(Q, 256);
+    if (4 * t >= 3 * 256 * cdiv(t, 256)) { pl.tile = kTile256; bp = bq = 256; }
+  }
+  pl.direct = (pl.tile == kTile256 || pl.tile == kTile128 || pl.tile == kTile64) && lin_direct(prod, bs, P, Q, K);
   const int64_t tiles = cdiv(P, bp) * cdiv(Q, bq);
   int64_t splits = 1;
   if (tiles < 256 && steps >= 8) splits = std::min(cdiv(512, tiles), steps / 4);
@@ -140,14 +144,19 @@ int run_linear(int act, int64_t rows, int64_t K, int64_t N, const void* X, const
   const LinPlan pl = lin_plan(kLinForward, sizeof(T), rows, N, K);
   LinGemmParams p = lin_params(pl, rows, N, K, X, W, ws);
   p.bias = bias; p.res = res; p.out = out; p.pre = pre; p.act = act;
-  if (pl.strip) HIPTRY(launch_lin_rows<T>(p, kLinForward, pl.strip, nullptr, FLAREPP_ACT_NONE, s));
+  if (pl.strip) HIPTRY(launch_lin_rows<T>(p, kLinForward, pl.strip, s));
   else HIPTRY(launch_lin_gemm<T>(p, kLinForward, pl.tile, pl.direct, s));
   if (p.part) HIPTRY(launch_lin_finish<T>(p, s));
   return api_ok();
 }
 
+// From these tokens on the one-pass backward has chunks enough for every CU
+constexpr int64_t kLinBwdFrom = 8192;
+
 struct LinBwdWs {
   LinPlan dx, dw;
+  bool pass, fused;  // one pass over the tokens; dX in it
+  int kt, nt;
   void *dp, *dp_lo, *part;
   float* bias_part;
   int64_t bias_ld, chunk;
@@ -166,7 +175,14 @@ LinBwdWs lin_bwd_ws(void* base, int dtype, int act, int64_t rows, int64_t K, int
     if (dtype == FLAREPP_BF16) w.dp_lo = cv.take(bs * rows * N);
   }
   w.chunk = std::max<int64_t>(64, cdiv(rows, 512));
+  w.pass = dtype == FLAREPP_BF16 && rows >= kLinBwdFrom && lin_bwd_tile(K, N, w.kt, w.nt, w.fused);
+  if (w.pass) {  // a workgroup per CU, of 256 tokens at least (its partial sums are as many bytes)
+    const int64_t tiles = (K / w.kt) * (N / w.nt);
+    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, rows / 256));
+    w.chunk = cdiv(cdiv(rows, groups), 32) * 32;
+  }
   w.nchunks = (int)cdiv(rows, w.chunk);
+  if (w.pass) w.dw.part_bytes = std::max(w.dw.part_bytes, sizeof(float) * w.nchunks * w.dw.part_stride);
   w.bias_ld = cdiv(N, 4) * 4;
   w.bias_part = static_cast<float*>(cv.take(sizeof(float) * w.nchunks * w.bias_ld));
   // the sums per split of the two products, one after the other
@@ -180,6 +196,28 @@ int run_linear_backward(int dtype, int act, int64_t rows, int64_t K, int64_t N, 
                         const void* dOut, void* dX, float* dW, float* dbias, void* ws, hipStream_t s) {
   const LinBwdWs w = lin_bwd_ws(ws, dtype, act, rows, K, N);
   const void* dp = dOut;
+  if (w.pass && dW) {
+    LinBwdParams p{};
+    p.x = X; p.w = W; p.pre = pre; p.dout = dOut;
+    p.dx = w.fused ? dX : nullptr;
+    p.hi = !w.fused && dX ? w.dp : nullptr;
+    p.part = static_cast<float*>(w.part); p.part_stride = w.dw.part_stride;
+    p.bias_part = dbias ? w.bias_part : nullptr; p.bias_ld = w.bias_ld;
+    p.T = rows; p.K = K; p.N = N; p.chunk = w.chunk; p.nchunks = w.nchunks; p.act = act;
+    HIPTRY(launch_lin_bwd(p, w.kt, w.nt, w.fused, s));
+    LinSumParams sums{};
+    sums.job[sums.njobs++] = {p.part, p.part_stride, K * N, w.nchunks, dW};
+    if (dbias) sums.job[sums.njobs++] = {w.bias_part, w.bias_ld, N, w.nchunks, dbias};
+    HIPTRY(launch_lin_sum(sums, s));
+    if (dX && !w.fused) {
+      LinGemmParams q = lin_params(w.dx, rows, K, N, act != FLAREPP_ACT_NONE ? w.dp : dOut, W, w.part);
+      q.out = dX;
+      if (w.dx.strip) HIPTRY(launch_lin_rows<T>(q, kLinInput, w.dx.strip, s));
+      else HIPTRY(launch_lin_gemm<T>(q, kLinInput, w.dx.tile, w.dx.direct, s));
+      if (q.part) HIPTRY(launch_lin_finish<T>(q, s));
+    }
+    return api_ok();
+  }
   if (act != FLAREPP_ACT_NONE || dbias) {
     LinSlopeParams p{};
     p.dout = dOut; p.pre = pre; p.act = act; p.T = rows; p.N = N;
@@ -195,12 +233,8 @@ int run_linear_backward(int dtype, int act, int64_t rows, int64_t K, int64_t N, 
   if (dX) {
     LinGemmParams p = lin_params(w.dx, rows, K, N, dp, W, w.part);
     p.out = dX;
-    if (w.dx.strip) {
-      p.l = dOut;
-      HIPTRY(launch_lin_rows<T>(p, kLinInput, w.dx.strip, pre, act, s));
-    } else {
-      HIPTRY(launch_lin_gemm<T>(p, kLinInput, w.dx.tile, w.dx.direct, s));
-    }
+    if (w.dx.strip) HIPTRY(launch_lin_rows<T>(p, kLinInput, w.dx.strip, s));
+    else HIPTRY(launch_lin_gemm<T>(p, kLinInput, w.dx.tile, w.dx.direct, s));
     if (p.part) HIPTRY(launch_lin_finish<T>(p, s));
   }
   LinSumParams sums{};

@@ -7,11 +7,11 @@ namespace flarepp {
 namespace {
 
 // ---- the product -------------------------------------------------------------------
-template <typename T, int PROD, bool LO, int BP, int BQ, int WP, int WQ, bool DIRECT, int NBUF>
+template <typename T, int PROD, bool LO, int BP, int BQ, int WP, int WQ, bool DIRECT, int NBUF, int KB>
 __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
   constexpr bool LT = lin_l_t(PROD), RT = lin_r_t(PROD);
-  using L = Tile<T, LT, BP>;
-  using R = Tile<T, RT, BQ>;
+  using L = Tile<T, LT, BP, KB>;
+  using R = Tile<T, RT, BQ, KB>;
   constexpr int EPC = L::EPC, BK = L::BK, NP = BP / WP / 32, NQ = BQ / WQ / 32, NW = WP * WQ, NT = 64 * NW;
   constexpr int BUF = L::BYTES + R::BYTES * (LO ? 2 : 1);
   __shared__ __attribute__((aligned(16))) char smem[BUF * NBUF];
@@ -66,30 +66,46 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
   if constexpr (DIRECT) {
     constexpr int IPW = BUF / 1024 / NW;  // 1 KiB copies of a step per wave
     static_assert(BUF % (1024 * NW) == 0, "whole copies per wave");
-    // rows and columns past the end repeat the last ones: their products are
-    // not stored, and reduction rows past the end are cleared below
+    // A copy's source: a base per step (uniform) and an offset per lane, the
+    // same in every step.  Rows and columns past the end repeat the last ones:
+    // their products are not stored; reduction rows past the end (of the last
+    // step) repeat too, and are cleared below.
+    uint32_t off[IPW];
+    auto offset = [&](int u, int64_t kleft) __attribute__((always_inline)) {
+      const int kib = wave * IPW + u;
+      const bool isl = kib < L::BYTES / 1024;
+      const int e = ((isl ? kib * 64 : kib * 64 - L::CHUNKS) + lane) % (isl ? L::CHUNKS : R::CHUNKS);
+      const int row = e / (isl ? L::CPR : R::CPR), slot = e % (isl ? L::CPR : R::CPR);
+      const int ch = isl ? L::swap(row, slot) : R::swap(row, slot);
+      const bool tr = isl ? LT : RT;
+      const int64_t n = isl ? p.P - p0 : p.Q - q0, ld = isl ? lld : rld;
+      const int64_t r = min((int64_t)row, (tr ? kleft : n) - 1), col = tr ? min((int64_t)ch * EPC, n - EPC) : ch * EPC;
+      return (uint32_t)((r * ld + col) * sizeof(T));
+    };
+#pragma unroll
+    for (int u = 0; u < IPW; ++u) off[u] = offset(u, BK);
+    // (bytes, as scalars: they are the uniform bases of the copies)
+    int64_t lat = scalar64((int64_t)(lsrc + (LT ? k0 * lld + p0 : p0 * lld + k0)));
+    int64_t rat = scalar64((int64_t)(rsrc + (RT ? k0 * rld + q0 : q0 * rld + k0)));
+    int64_t rlo_at = LO ? scalar64((int64_t)(rlo + (RT ? k0 * rld + q0 : q0 * rld + k0))) : 0;
+    const int64_t ladd = (LT ? BK * lld : BK) * (int64_t)sizeof(T), radd = (RT ? BK * rld : BK) * (int64_t)sizeof(T);
     auto issue = [&](int s) __attribute__((always_inline)) {
       if (s >= nsteps) return;
       char* dst = smem + s % NBUF * BUF;
-      const int64_t k = k0 + (int64_t)s * BK;
+      const int64_t kleft = p.K - k0 - (int64_t)s * BK;
+      if (LT && RT && kleft < BK) {
+#pragma unroll
+        for (int u = 0; u < IPW; ++u) off[u] = offset(u, kleft);
+      }
 #pragma unroll
       for (int u = 0; u < IPW; ++u) {
         const int kib = wave * IPW + u;
-        const T* src;
-        if (kib < L::BYTES / 1024) {
-          const int e = kib * 64 + lane, row = e / L::CPR, ch = L::swap(row, e % L::CPR);
-          if constexpr (LT) src = lsrc + min(k + row, p.K - 1) * lld + min(p0 + (int64_t)ch * EPC, p.P - EPC);
-          else src = lsrc + min(p0 + row, p.P - 1) * lld + k + ch * EPC;
-        } else {
-          const int e0 = (kib - L::BYTES / 1024) * 64 + lane;
-          const bool lo = LO && e0 >= R::CHUNKS;
-          const int e = lo ? e0 - R::CHUNKS : e0, row = e / R::CPR, ch = R::swap(row, e % R::CPR);
-          const T* base = lo ? rlo : rsrc;
-          if constexpr (RT) src = base + min(k + row, p.K - 1) * rld + min(q0 + (int64_t)ch * EPC, p.Q - EPC);
-          else src = base + min(q0 + row, p.Q - 1) * rld + k + ch * EPC;
-        }
-        lds_copy16(src, dst + kib * 1024);
+        const int64_t base = kib < L::BYTES / 1024 ? lat : LO && kib >= (L::BYTES + R::BYTES) / 1024 ? rlo_at : rat;
+        lds_copy16_at(reinterpret_cast<const void*>(base), off[u], dst + kib * 1024);
       }
+      lat += ladd;
+      rat += radd;
+      if (LO) rlo_at += radd;
     };
     for (int s = 0; s < NBUF - 1; ++s) issue(s);
     for (int s = 0; s < nsteps; ++s) {
@@ -155,13 +171,13 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
     }
   }
 
-#pragma unroll
-  for (int j = 0; j < NP; ++j) {
+  static_for<0, NP>([&](auto jc) __attribute__((always_inline)) {
+    constexpr int j = decltype(jc)::value;
     const int64_t row = p0 + 32 * (wp * NP + j) + c;
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
+    static_for<0, NQ>([&](auto ic) __attribute__((always_inline)) {
+      constexpr int i = decltype(ic)::value;
       const int64_t qb = q0 + 32 * (wq * NQ + i);
-      if (qb >= p.Q) continue;
+      if (qb >= p.Q) return;
       if (!p.part) {
         if (p.Q % EPC == 0 && qb + 32 <= p.Q) {
           const int64_t at = min(row, p.P - 1) * p.Q + qb;
@@ -182,7 +198,7 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
         } else {
           epilogue_parts<T>(acc[i][j], p, row, qb);
         }
-        continue;
+        return;
       }
       const bool whole = p.Q % 4 == 0;
 #pragma unroll
@@ -193,8 +209,8 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
         for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * u + e];
         if (row < p.P && q < p.Q) store_part(p.part + z * p.part_stride, p.Q, row, q, v, whole);
       }
-    }
-  }
+    });
+  });
 }
 
 // ---- epilogue of a product whose reduction was split ----------------------------------
@@ -269,42 +285,51 @@ __global__ __launch_bounds__(256) void k_linear_slope(LinSlopeParams p, int cl_l
 }
 
 // ---- sums of partials in a fixed order ---------------------------------------------------
-// 64 outputs per workgroup, four waves that each sum a run of the splits.
+// 64 outputs per workgroup: 16 lanes of four outputs, 16 groups of lanes that
+// each sum every 16th split with eight loads in flight, then the groups in order.
 __global__ __launch_bounds__(256) void k_linear_sum(LinSumParams p, int64_t first1) {
-  __shared__ float sums[4][64];
+  __shared__ f32x4 sums[16][16];
   const int jb = p.njobs > 1 && (int64_t)blockIdx.x >= first1 ? 1 : 0;
   const LinSumJob& j = p.job[jb];
-  const int lane = lane_id(), wave = wave_id();
-  const int64_t i = ((int64_t)blockIdx.x - (jb ? first1 : 0)) * 64 + lane;
-  const int per = (j.splits + 3) / 4, s0 = wave * per, s1 = min(j.splits, s0 + per);
-  float s = 0.f;
-  if (i < j.n) {
+  const int l = threadIdx.x & 15, gr = threadIdx.x >> 4;
+  const int64_t i = (((int64_t)blockIdx.x - (jb ? first1 : 0)) * 16 + l) * 4;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (i < j.n) {  // (strides are multiples of four: the last vector may read padding)
     const float* x = j.part + i;
-    int z = s0;
-    for (; z + 8 <= s1; z += 8) {
-      float v[8];
+    for (int z = gr; z < j.splits; z += 128) {
+      f32x4 v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = x[(z + e) * j.stride];
+      for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const f32x4*>(x + min(z + 16 * e, j.splits - 1) * j.stride);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += v[e];
+      for (int e = 0; e < 8; ++e)
+        if (z + 16 * e < j.splits) s += v[e];
     }
-    for (; z < s1; ++z) s += x[z * j.stride];
   }
-  sums[wave][lane] = s;
+  sums[gr][l] = s;
   __syncthreads();
-  if (wave == 0 && i < j.n) j.out[i] = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+  if (gr == 0 && i < j.n) {
+    s = sums[0][l];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) s += sums[e][l];
+    if (i + 4 <= j.n) *reinterpret_cast<f32x4*>(j.out + i) = s;
+    else
+      for (int e = 0; i + e < j.n; ++e) j.out[i + e] = s[e];
+  }
 }
 
-template <typename T, int PROD, bool LO, int BP, int BQ, int WP, int WQ, bool DIRECT, int NBUF>
+template <typename T, int PROD, bool LO, int BP, int BQ, int WP, int WQ, bool DIRECT, int NBUF, int KB = 128>
 hipError_t launch_tile(const LinGemmParams& p, hipStream_t s) {
   const int64_t total = (p.P + BP - 1) / BP * ((p.Q + BQ - 1) / BQ) * p.splits;
   const int64_t grid = (total + 7) / 8 * 8;
-  k_linear<T, PROD, LO, BP, BQ, WP, WQ, DIRECT, NBUF><<<dim3((unsigned)grid), 64 * WP * WQ, 0, s>>>(p);
+  k_linear<T, PROD, LO, BP, BQ, WP, WQ, DIRECT, NBUF, KB><<<dim3((unsigned)grid), 64 * WP * WQ, 0, s>>>(p);
   return hipGetLastError();
 }
 
 template <typename T, int PROD, bool LO>
 hipError_t launch_prod(const LinGemmParams& p, int tile, bool direct, hipStream_t s) {
+  if constexpr (sizeof(T) == 2 && PROD != kLinWeight) {
+    if (tile == kTile256) return launch_tile<T, PROD, LO, 256, 256, 2, 4, true, 2>(p, s);
+  }
   switch (tile) {
     case kTile128:
       return direct ? launch_tile<T, PROD, LO, 128, 128, 2, 2, true, 2>(p, s) : launch_tile<T, PROD, LO, 128, 128, 2, 2, false, 2>(p, s);

@@ -60,19 +60,41 @@ template <typename Fn> __device__ __forceinline__ void with_act(int act, Fn f) {
   else f(ActC<kActNone>{});
 }
 
+// f(0), .. f(N - 1) with the index as a constant
+template <int I, int N, typename Fn> __device__ __forceinline__ void static_for(Fn f) {
+  if constexpr (I < N) {
+    f(ActC<I>{});
+    static_for<I + 1, N>(f);
+  }
+}
+
+// A value every lane agrees on, in scalar registers
+__device__ __forceinline__ int64_t scalar64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+// lds_copy16 from a wave-uniform base and a byte offset per lane
+__device__ __forceinline__ void lds_copy16_at(const void* base, uint32_t off, char* dst) {
+  const unsigned to = __builtin_amdgcn_readfirstlane(
+      (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)dst);
+  unsigned m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "v"(off), "s"(scalar64((int64_t)base)), "s"(to) : "memory");
+}
+
 // ---- operand tiles in LDS ----------------------------------------------------------
-// A step holds 128 bytes of the reduction of every row.  k-contiguous operands
-// lie as [ROWS][128 bytes] with a row's eight 16-byte chunks permuted by the
-// row, the others as [k][ROWS] with groups of four chunks permuted by k for the
-// transposing reads: the 256 bytes of a read's turn (one chunk of 16 rows; 64
+// A step holds KB bytes (128 or 64) of the reduction of every row.
+// k-contiguous operands lie as [ROWS][KB] with a row's 16-byte chunks permuted by
+// the row, the others as [k][ROWS] with groups of four chunks permuted by k for
+// the transposing reads: the 256 bytes of a read's turn (one chunk of 16 rows; 64
 // bytes of four k) fall in different banks.
-template <typename T, bool TR, int ROWS> struct Tile {
-  static constexpr int EPC = 16 / (int)sizeof(T), BK = 128 / (int)sizeof(T);
-  static constexpr int CPR = TR ? ROWS / EPC : 8;  // chunks of a stored row
-  static constexpr int BYTES = ROWS * 128, CHUNKS = ROWS * 8;
+template <typename T, bool TR, int ROWS, int KB = 128> struct Tile {
+  static constexpr int EPC = 16 / (int)sizeof(T), BK = KB / (int)sizeof(T);
+  static constexpr int CPR = TR ? ROWS / EPC : KB / 16;  // chunks of a stored row
+  static constexpr int BYTES = ROWS * KB, CHUNKS = BYTES / 16;
   // the source chunk that LDS slot s of stored row `row` holds (an involution)
   static __device__ __forceinline__ int swap(int row, int s) {
-    if constexpr (!TR) return s ^ (row >> 1 & 7);
+    if constexpr (!TR) return s ^ (row / (256 / KB) & (KB / 16 - 1));
     else if constexpr (sizeof(T) == 4) return s;
     else return s ^ (ROWS >= 128 ? 4 * (row & 3) : ROWS == 64 ? 4 * (row >> 1 & 1) : 0);
   }
@@ -82,11 +104,11 @@ template <typename T, bool TR, int ROWS> struct Tile {
     const int lane = lane_id(), g = lane >> 5, c = lane & 31;
     if constexpr (!TR && sizeof(T) == 2) {
       const int row = 32 * blk + c;
-      return load_frag(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 2 * ks + g) * 16));
+      return load_frag(reinterpret_cast<const T*>(buf + row * KB + swap(row, 2 * ks + g) * 16));
     } else if constexpr (!TR) {
       const int row = 32 * blk + c;
-      return join<T>(load_half(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 4 * ks + 2 * g) * 16)),
-                     load_half(reinterpret_cast<const T*>(buf + row * 128 + swap(row, 4 * ks + 2 * g + 1) * 16)));
+      return join<T>(load_half(reinterpret_cast<const T*>(buf + row * KB + swap(row, 4 * ks + 2 * g) * 16)),
+                     load_half(reinterpret_cast<const T*>(buf + row * KB + swap(row, 4 * ks + 2 * g + 1) * 16)));
     } else if constexpr (sizeof(T) == 2) {
       const int i16 = lane & 15, k = 16 * ks + 8 * g + (i16 >> 2);
       const int s = 4 * blk + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);

@@ -10,15 +10,15 @@ namespace {
 // LDS: persistent workgroups of eight waves, each wave walking tiles of 32 rows
 // on its own.  Rows come straight from memory as MFMA fragments, a segment of SEG
 // 16-element steps ahead, so every element of L passes a CU once and no barrier
-// follows the weights' copy.  SLOPE: L = l * act'(pre), formed in registers.
+// follows the weights' copy.
 // STEPS: K is whole steps of 16 (else rows are read by single elements).
 // WHOLE: Q is whole blocks of 32.
-template <typename T, bool RT, int NB, bool SLOPE, bool STEPS, bool WHOLE>
-__global__ __launch_bounds__(512) void k_linear_rows(LinGemmParams p, const void* slope_pre, int slope_act) {
+template <typename T, bool RT, int NB, bool STEPS, bool WHOLE>
+__global__ __launch_bounds__(512) void k_linear_rows(LinGemmParams p) {
   using F = typename Frag<T>::type;
   using R = Tile<T, RT, NB>;
   constexpr int EPC = R::EPC, BK = R::BK, NQ = NB / 32, KPB = BK / 16;  // steps of a buffer of BK
-  constexpr int SEG = !STEPS ? 1 : SLOPE || sizeof(T) == 4 || NB == 256 ? 4 : 8;
+  constexpr int SEG = !STEPS ? 1 : sizeof(T) == 4 || NB == 256 ? 4 : 8;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int lane = lane_id(), wave = wave_id(), g = lane >> 5, c = lane & 31;
   const int64_t q0 = (int64_t)blockIdx.y * NB;
@@ -58,26 +58,22 @@ __global__ __launch_bounds__(512) void k_linear_rows(LinGemmParams p, const void
 
   struct Rows {
     F x[SEG];
-    F y[SLOPE ? SEG : 1];
   };
   auto load = [&](Rows& r, int64_t t, int seg) __attribute__((always_inline)) {
     const int64_t at = min(t * 32 + c, p.P - 1) * K;
     const T* l = static_cast<const T*>(p.l) + at;
-    const T* y = SLOPE ? static_cast<const T*>(slope_pre) + at : nullptr;
 #pragma unroll
     for (int j = 0; j < SEG; ++j) {
       const int k = (seg * SEG + j) * 16 + 8 * g;
       if constexpr (STEPS) {
         const int kc = min(k, K - 16 + 8 * g);  // steps past the end are not used
         r.x[j] = load_frag(l + kc);
-        if constexpr (SLOPE) r.y[j] = load_frag(y + kc);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int kc = min(k + e, K - 1);
           const T v = l[kc];
           r.x[j][e] = k + e < K ? v : from_f32<T>(0.f);
-          if constexpr (SLOPE) r.y[j][e] = y[kc];
         }
       }
     }
@@ -101,19 +97,9 @@ __global__ __launch_bounds__(512) void k_linear_rows(LinGemmParams p, const void
     if (ntile < tiles) load(next, ntile, nxt);
     auto step = [&](int j) __attribute__((always_inline)) {
       const int ks = seg * SEG + j;
-      F x = now.x[j];
-      if constexpr (SLOPE) {
-        with_act(slope_act, [&](auto act) __attribute__((always_inline)) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float v = to_f32(x[e]) * slope<decltype(act)::value>(to_f32(now.y[j][e]));
-            x[e] = from_f32<T>(STEPS || ks * 16 + 8 * g + e < K ? v : 0.f);
-          }
-        });
-      }
 #pragma unroll
       for (int i = 0; i < NQ; ++i)
-        mma(acc[i], RT ? R::frag(smem, i, ks) : R::frag(smem + ks / KPB * R::BYTES, i, ks % KPB), x);
+        mma(acc[i], RT ? R::frag(smem, i, ks) : R::frag(smem + ks / KPB * R::BYTES, i, ks % KPB), now.x[j]);
     };
 #pragma unroll
     for (int j = 0; j < SEG; ++j)
@@ -155,26 +141,26 @@ __global__ __launch_bounds__(512) void k_linear_rows(LinGemmParams p, const void
   }
 }
 
-template <typename T, bool RT, int NB, bool SLOPE, bool STEPS, bool WHOLE>
-hipError_t launch_strip(const LinGemmParams& p, const void* pre, int act, hipStream_t s) {
+template <typename T, bool RT, int NB, bool STEPS, bool WHOLE>
+hipError_t launch_strip(const LinGemmParams& p, hipStream_t s) {
   const int64_t tiles = (p.P + 31) / 32, strips = (p.Q + NB - 1) / NB;
   const size_t lds = lin_rows_lds(sizeof(T), NB, p.K);
   const int64_t groups = std::min<int64_t>((tiles + 7) / 8, std::max<int64_t>(1, 256 / strips));
-  auto* kernel = k_linear_rows<T, RT, NB, SLOPE, STEPS, WHOLE>;
+  auto* kernel = k_linear_rows<T, RT, NB, STEPS, WHOLE>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
-  kernel<<<dim3((unsigned)groups, (unsigned)strips), 512, lds, s>>>(p, pre, act);
+  kernel<<<dim3((unsigned)groups, (unsigned)strips), 512, lds, s>>>(p);
   return hipGetLastError();
 }
 
-template <typename T, bool RT, bool SLOPE>
-hipError_t launch_form(const LinGemmParams& p, int strip, const void* pre, int act, hipStream_t s) {
+template <typename T, bool RT>
+hipError_t launch_form(const LinGemmParams& p, int strip, hipStream_t s) {
   const bool whole = p.Q % 32 == 0, steps = p.K % 16 == 0;
   if constexpr (RT) {
-    if (!whole && strip == 32) return launch_strip<T, RT, 32, SLOPE, true, false>(p, pre, act, s);
-    if (!whole) return launch_strip<T, RT, 64, SLOPE, true, false>(p, pre, act, s);
+    if (!whole && strip == 32) return launch_strip<T, RT, 32, true, false>(p, s);
+    if (!whole) return launch_strip<T, RT, 64, true, false>(p, s);
   }
-#define FORM(NB) return steps ? launch_strip<T, RT, NB, SLOPE, true, true>(p, pre, act, s) : launch_strip<T, RT, NB, SLOPE, false, true>(p, pre, act, s)
+#define FORM(NB) return steps ? launch_strip<T, RT, NB, true, true>(p, s) : launch_strip<T, RT, NB, false, true>(p, s)
   if constexpr (sizeof(T) == 2) {
     if (strip == 256) FORM(256);
     if (strip == 128) FORM(128);
@@ -205,11 +191,10 @@ int lin_rows_strip(int prod, int elem_bytes, int64_t Q, int64_t K) {
 }
 
 template <typename T>
-hipError_t launch_lin_rows(const LinGemmParams& p, int prod, int strip, const void* pre, int act, hipStream_t s) {
-  if (prod == kLinForward) return launch_form<T, true, false>(p, strip, nullptr, kActNone, s);
-  return act == kActNone ? launch_form<T, false, false>(p, strip, nullptr, act, s) : launch_form<T, false, true>(p, strip, pre, act, s);
+hipError_t launch_lin_rows(const LinGemmParams& p, int prod, int strip, hipStream_t s) {
+  return prod == kLinForward ? launch_form<T, true>(p, strip, s) : launch_form<T, false>(p, strip, s);
 }
-template hipError_t launch_lin_rows<float>(const LinGemmParams&, int, int, const void*, int, hipStream_t);
-template hipError_t launch_lin_rows<__bf16>(const LinGemmParams&, int, int, const void*, int, hipStream_t);
+template hipError_t launch_lin_rows<float>(const LinGemmParams&, int, int, hipStream_t);
+template hipError_t launch_lin_rows<__bf16>(const LinGemmParams&, int, int, hipStream_t);
 
 }  // namespace flarepp

@@ -169,6 +169,50 @@ def test_backward(shape, dtype):
     _check_backward(X, W, pre, d, "gelu", dtype, fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_GELU))
 
 
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("shape", [(8192, 64, 64), (8193, 64, 128), (8223, 64, 256), (9000, 128, 64), (8200, 128, 128),
+                                   (8500, 128, 256), (8211, 256, 64), (8300, 256, 128), (8205, 256, 256), (8199, 512, 384),
+                                   (8250, 384, 128)], ids=str)
+def test_backward_over_many_tokens(shape, act):
+    """The one-pass backward: every tile of inputs and outputs, ragged ends of
+    the last chunk and step, dX inside of the pass and after it."""
+    X, W, _, pre, d = _inputs(*shape, "bf16", seed=10)
+    pre = None if act == "none" else pre
+    g = fp.flarepp_linear_backward(X, W, d, pre=pre, act=ACTS[act])
+    _check_backward(X, W, pre, d, act, "bf16", g)
+    bad = X.clone()
+    bad[-1, 1] = float("inf")  # the last row, which a ragged step repeats
+    h = fp.flarepp_linear_backward(bad, W, d, pre=pre, act=ACTS[act])
+    assert torch.equal(h["dX"], g["dX"]) and torch.equal(h["dbias"], g["dbias"])
+    keep = [k for k in range(shape[1]) if k != 1]
+    assert torch.equal(h["dW"][keep], g["dW"][keep])
+    want = d[-1].double() if act == "none" else None
+    if want is not None:
+        assert torch.equal(torch.isposinf(h["dW"][1]), want > 0) and torch.equal(torch.isneginf(h["dW"][1]), want < 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(8192, 16, 32), (8195, 3, 64), (8200, 5, 256), (8193, 64, 4), (8200, 144, 33), (8192, 128, 256),
+                                   (8300, 288, 128), (8192, 512, 256), (8192, 512, 512), (8201, 30, 96)], ids=str)
+def test_forward_over_many_rows(shape, dtype):
+    """The rows kernel: every strip width, short rows, narrow outputs, two strips."""
+    T, K, N = shape
+    X, W, b, r, _ = _inputs(T, K, N, dtype, seed=11)
+    _check_forward(X, W, b, r, "silu", dtype, *fp.flarepp_linear_forward(X, W, b, act=fp.ACT_SILU, residual=r, keep_pre=True))
+    _check_forward(X, W, None, None, "none", dtype, fp.flarepp_linear_forward(X, W), None)
+
+
+@pytest.mark.parametrize("shape", [(16500, 1024, 1032), (12544, 128, 1024)], ids=str)
+def test_wide_tiles(shape):
+    X, W, b, r, d = _inputs(*shape, "bf16", seed=12)
+    rows = slice(-300, None)  # the reference of some rows is enough: rows are independent
+    out, pre = fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, residual=r, keep_pre=True)
+    for sl in (slice(0, 300), rows):
+        _check_forward(X[sl], W, b, r[sl], "gelu", "bf16", out[sl], pre[sl])
+        g = fp.flarepp_linear_backward(X, W, d, want_dW=False, want_dbias=False)
+        _check_backward(X[sl], W, None, d[sl], "none", "bf16", {"dX": g["dX"][sl]})
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("act", list(ACTS))
 @pytest.mark.parametrize("shape", [(700, 64, 136), (2100, 37, 9)], ids=str)
