@@ -70,7 +70,7 @@ struct LinBwdParams {
   int64_t T, K, N, chunk;
   int nchunks, act;
 };
-bool lin_bwd_tile(int64_t K, int64_t N, int& kt, int& nt, bool& fused);
+bool lin_bwd_tile(int64_t K, int64_t N, int act, int& kt, int& nt, bool& fused);
 hipError_t launch_lin_bwd(const LinBwdParams&, int kt, int nt, bool fused, hipStream_t);
 
 // out[i] = sum_s part[s * stride + i], i < n: two independent jobs in a launch

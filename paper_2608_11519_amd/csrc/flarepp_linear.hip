@@ -64,48 +64,54 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
   };
 
   if constexpr (DIRECT) {
-    constexpr int IPW = BUF / 1024 / NW;  // 1 KiB copies of a step per wave
-    static_assert(BUF % (1024 * NW) == 0, "whole copies per wave");
+    // 1 KiB copies of a step per wave: L, then R (and its low part)
+    constexpr int LC = L::BYTES / 1024 / NW, RC = R::BYTES / 1024 / NW, IPW = LC + RC * (LO ? 2 : 1);
+    static_assert(L::BYTES % (1024 * NW) == 0 && R::BYTES % (1024 * NW) == 0, "whole copies per wave");
     // A copy's source: a base per step (uniform) and an offset per lane, the
     // same in every step.  Rows and columns past the end repeat the last ones:
     // their products are not stored; reduction rows past the end (of the last
     // step) repeat too, and are cleared below.
-    uint32_t off[IPW];
-    auto offset = [&](int u, int64_t kleft) __attribute__((always_inline)) {
-      const int kib = wave * IPW + u;
-      const bool isl = kib < L::BYTES / 1024;
-      const int e = ((isl ? kib * 64 : kib * 64 - L::CHUNKS) + lane) % (isl ? L::CHUNKS : R::CHUNKS);
-      const int row = e / (isl ? L::CPR : R::CPR), slot = e % (isl ? L::CPR : R::CPR);
-      const int ch = isl ? L::swap(row, slot) : R::swap(row, slot);
-      const bool tr = isl ? LT : RT;
-      const int64_t n = isl ? p.P - p0 : p.Q - q0, ld = isl ? lld : rld;
-      const int64_t r = min((int64_t)row, (tr ? kleft : n) - 1), col = tr ? min((int64_t)ch * EPC, n - EPC) : ch * EPC;
-      return (uint32_t)((r * ld + col) * sizeof(T));
-    };
+    uint32_t loff[LC], roff[RC];
+    auto offsets = [&](int64_t kleft) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < IPW; ++u) off[u] = offset(u, BK);
-    // (bytes, as scalars: they are the uniform bases of the copies)
-    int64_t lat = scalar64((int64_t)(lsrc + (LT ? k0 * lld + p0 : p0 * lld + k0)));
-    int64_t rat = scalar64((int64_t)(rsrc + (RT ? k0 * rld + q0 : q0 * rld + k0)));
-    int64_t rlo_at = LO ? scalar64((int64_t)(rlo + (RT ? k0 * rld + q0 : q0 * rld + k0))) : 0;
+      for (int u = 0; u < LC; ++u) {
+        const int e = (wave * LC + u) * 64 + lane, row = e / L::CPR, ch = L::swap(row, e % L::CPR);
+        const int64_t n = p.P - p0, r = min((int64_t)row, (LT ? kleft : n) - 1);
+        loff[u] = (uint32_t)((r * lld + (LT ? min((int64_t)ch * EPC, n - EPC) : ch * EPC)) * sizeof(T));
+      }
+#pragma unroll
+      for (int u = 0; u < RC; ++u) {
+        const int e = (wave * RC + u) * 64 + lane, row = e / R::CPR, ch = R::swap(row, e % R::CPR);
+        const int64_t n = p.Q - q0, r = min((int64_t)row, (RT ? kleft : n) - 1);
+        roff[u] = (uint32_t)((r * rld + (RT ? min((int64_t)ch * EPC, n - EPC) : ch * EPC)) * sizeof(T));
+      }
+    };
+    offsets(BK);
+    const int64_t rfirst = (RT ? k0 * rld + q0 : q0 * rld + k0);
+    int64_t lat = scalar64((int64_t)(lsrc + (LT ? k0 * lld + p0 : p0 * lld + k0)));  // bytes
+    int64_t rat = scalar64((int64_t)(rsrc + rfirst));
+    int64_t rlo_at = LO ? scalar64((int64_t)(rlo + rfirst)) : 0;
     const int64_t ladd = (LT ? BK * lld : BK) * (int64_t)sizeof(T), radd = (RT ? BK * rld : BK) * (int64_t)sizeof(T);
     auto issue = [&](int s) __attribute__((always_inline)) {
       if (s >= nsteps) return;
       char* dst = smem + s % NBUF * BUF;
-      const int64_t kleft = p.K - k0 - (int64_t)s * BK;
-      if (LT && RT && kleft < BK) {
-#pragma unroll
-        for (int u = 0; u < IPW; ++u) off[u] = offset(u, kleft);
+      if constexpr (LT && RT) {
+        const int64_t kleft = p.K - k0 - (int64_t)s * BK;
+        if (kleft < BK) offsets(kleft);
       }
 #pragma unroll
-      for (int u = 0; u < IPW; ++u) {
-        const int kib = wave * IPW + u;
-        const int64_t base = kib < L::BYTES / 1024 ? lat : LO && kib >= (L::BYTES + R::BYTES) / 1024 ? rlo_at : rat;
-        lds_copy16_at(reinterpret_cast<const void*>(base), off[u], dst + kib * 1024);
+      for (int u = 0; u < LC; ++u) lds_copy16_at(reinterpret_cast<const void*>(lat), loff[u], dst + (wave * LC + u) * 1024);
+#pragma unroll
+      for (int u = 0; u < RC; ++u)
+        lds_copy16_at(reinterpret_cast<const void*>(rat), roff[u], dst + L::BYTES + (wave * RC + u) * 1024);
+      if constexpr (LO) {
+#pragma unroll
+        for (int u = 0; u < RC; ++u)
+          lds_copy16_at(reinterpret_cast<const void*>(rlo_at), roff[u], dst + L::BYTES + R::BYTES + (wave * RC + u) * 1024);
+        rlo_at += radd;
       }
       lat += ladd;
       rat += radd;
-      if (LO) rlo_at += radd;
     };
     for (int s = 0; s < NBUF - 1; ++s) issue(s);
     for (int s = 0; s < nsteps; ++s) {

@@ -11,19 +11,18 @@ namespace flarepp {
 namespace {
 
 // ---- activations ---------------------------------------------------------------
-// Phi(-|y|), the normal distribution's lower tail, by Abramowitz and Stegun
-// 7.1.26: 1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), absolute
-// error 1.5e-7 in erf.  The tail form keeps it free of cancellation for negative y.
-__device__ __forceinline__ float normal_tail(float y, float& gauss) {
-  const float x = __builtin_fabsf(y) * 0.70710678f;
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
-  gauss = __builtin_amdgcn_exp2f(y * y * -0.72134752f);  // exp(-y^2 / 2)
-  float q = 1.061405429f;
-  q = __builtin_fmaf(q, t, -1.453152027f);
-  q = __builtin_fmaf(q, t, 1.421413741f);
-  q = __builtin_fmaf(q, t, -0.284496736f);
-  q = __builtin_fmaf(q, t, 0.254829592f);
-  return 0.5f * q * t * gauss;
+// Phi(y) - 1/2 and exp(-y^2 / 2) of the normal distribution, by Abramowitz and
+// Stegun 7.1.26: 1 - erf(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), absolute
+// error 1.5e-7 in erf (the coefficients are halved here).
+__device__ __forceinline__ float normal_half(float y, float& gauss) {
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678f, __builtin_fabsf(y), 1.f));
+  gauss = __builtin_amdgcn_exp2f(y * -0.72134752f * y);
+  float q = 0.5f * 1.061405429f;
+  q = __builtin_fmaf(q, t, 0.5f * -1.453152027f);
+  q = __builtin_fmaf(q, t, 0.5f * 1.421413741f);
+  q = __builtin_fmaf(q, t, 0.5f * -0.284496736f);
+  q = __builtin_fmaf(q, t, 0.5f * 0.254829592f);
+  return __builtin_copysignf(__builtin_fmaf(-q * t, gauss, 0.5f), y);
 }
 __device__ __forceinline__ float sigmoid(float y) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y * -1.44269504f));
@@ -32,8 +31,8 @@ template <int ACT> __device__ __forceinline__ float activate(float y) {
   if constexpr (ACT == kActRelu) return y < 0.f ? 0.f : y;  // a NaN stays
   if constexpr (ACT == kActGelu) {
     float gauss;
-    const float tail = normal_tail(y, gauss);
-    return y * (y < 0.f ? tail : 1.f - tail);
+    const float h = normal_half(y, gauss);
+    return __builtin_fmaf(y, h, 0.5f * y);
   }
   if constexpr (ACT == kActSilu) return y * sigmoid(y);
   return y;
@@ -42,8 +41,8 @@ template <int ACT> __device__ __forceinline__ float slope(float y) {
   if constexpr (ACT == kActRelu) return y > 0.f ? 1.f : 0.f;
   if constexpr (ACT == kActGelu) {
     float gauss;
-    const float tail = normal_tail(y, gauss);
-    return __builtin_fmaf(y * 0.39894228f, gauss, y < 0.f ? tail : 1.f - tail);
+    const float h = normal_half(y, gauss);
+    return __builtin_fmaf(y * 0.39894228f, gauss, 0.5f) + h;
   }
   if constexpr (ACT == kActSilu) {
     const float s = sigmoid(y);

@@ -54,8 +54,9 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
       const int kib = wave * XPW + u;
       if (kib >= XC) break;
       const int e = kib * 64 + lane, row = e / X::CPR, ch = X::swap(row, e % X::CPR);
-      const int64_t t = min(t0 + (int64_t)s * TS + row, p.T - 1);
-      lds_copy16(static_cast<const T*>(p.x) + t * p.K + c0 + ch * 8, smem + B::XAT + s % 3 * B::XB + kib * 1024);
+      const int64_t first = t0 + (int64_t)s * TS;
+      const uint32_t at = (uint32_t)min((int64_t)row, p.T - 1 - first) * (uint32_t)p.K + ch * 8;
+      lds_copy16_at(static_cast<const T*>(p.x) + first * p.K + c0, at * 2, smem + B::XAT + s % 3 * B::XB + kib * 1024);
     }
   };
   // this thread's chunks of dOut and pre: column chunk cc, rows r0 + j * RP
@@ -66,11 +67,16 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
     bf16x8 d[NJ], y[SLOPE ? NJ : 1];
   };
   auto load_p = [&](Raw& r, int s) __attribute__((always_inline)) {
+    // a uniform base per step and an offset per lane; rows past the end repeat the last one
+    const int64_t first = t0 + (int64_t)min(s, nsteps - 1) * TS;
+    const T* db = dout + first * p.N + n0;
+    const T* yb = SLOPE ? pre + first * p.N + n0 : nullptr;
+    const int last = (int)min(p.T - 1 - first, (int64_t)TS - 1);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int64_t at = min(t0 + (int64_t)s * TS + r0 + j * RP, p.T - 1) * p.N + n0 + cc * 8;
-      r.d[j] = load_frag(dout + at);
-      if constexpr (SLOPE) r.y[j] = load_frag(pre + at);
+      const uint32_t at = (uint32_t)min(r0 + j * RP, last) * (uint32_t)p.N + cc * 8;
+      r.d[j] = load_frag(db + at);
+      if constexpr (SLOPE) r.y[j] = load_frag(yb + at);
     }
   };
   float bias[8];
@@ -78,6 +84,7 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
   for (int e = 0; e < 8; ++e) bias[e] = 0.f;
   auto produce = [&](const Raw& r, int s) __attribute__((always_inline)) {
     char* buf = smem + B::PAT + (s & 1) * (B::PARTS * B::PB);
+    const bool ragged = t0 + (int64_t)(s + 1) * TS > t1;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const int row = r0 + j * RP;
@@ -91,7 +98,7 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
         });
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          v[e] = t < t1 ? v[e] : 0.f;
+          if (ragged) v[e] = t < t1 ? v[e] : 0.f;
           bias[e] += v[e];
           hi[e] = (__bf16)v[e];
           lo[e] = (__bf16)(v[e] - (float)hi[e]);
@@ -99,7 +106,7 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          hi[e] = t < t1 ? r.d[j][e] : (__bf16)0.f;
+          hi[e] = !ragged || t < t1 ? r.d[j][e] : (__bf16)0.f;
           bias[e] += (float)hi[e];
         }
       }
@@ -137,21 +144,7 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  for (int s = 0; s < nsteps; ++s) {
-    // the step's rows of X and its dP are in LDS, and every wave has left the
-    // buffers of the step before
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    issue_x(s + 2);
-    load_p(next, s + 2);
-    char* xb = smem + B::XAT + s % 3 * B::XB;
-    const char* pb = smem + B::PAT + (s & 1) * (B::PARTS * B::PB);
-    const int left = (int)min((int64_t)TS, t1 - t0 - (int64_t)s * TS);
-    if (left < TS) {  // rows past the end count as zero, also where X is not finite
-      for (int e = threadIdx.x; e < B::XB / 16; e += 512)
-        if (e / X::CPR >= left) reinterpret_cast<f32x4*>(xb)[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-      lds_barrier();
-    }
-    if (s + 1 < nsteps) produce(now, s + 1);
+  auto consume = [&](int s, const char* xb, const char* pb, int left) __attribute__((always_inline)) {
     if constexpr (DX) {
       // the step's dX: 32 inputs per wave; groups of KB waves take the steps in turn
       constexpr int GROUPS = 8 / B::KB;
@@ -160,10 +153,13 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
         f32x16 d;
 #pragma unroll
         for (int e = 0; e < 16; ++e) d[e] = 0.f;
+#pragma unroll 1  // (unrolled, the loads of all its steps would be in registers at once)
+        for (int b = 0; b < NT / 64; ++b) {
 #pragma unroll
-        for (int ks = 0; ks < NT / 16; ++ks) {
-          const bf16x8 l = load_frag(reinterpret_cast<const T*>(pb + c * NT * 2 + p_slot<NT>(c, 2 * ks + g) * 16));
-          mma(d, W::frag(smem + ks / 4 * W::BYTES, kb, ks % 4), l);
+          for (int k4 = 0; k4 < 4; ++k4) {
+            const bf16x8 l = load_frag(reinterpret_cast<const T*>(pb + c * NT * 2 + p_slot<NT>(c, 8 * b + 2 * k4 + g) * 16));
+            mma(d, W::frag(smem + b * W::BYTES, kb, k4), l);
+          }
         }
         if (c < left) {
           T* out = static_cast<T*>(p.dx) + (t0 + (int64_t)s * TS + c) * p.K + 32 * kb;
@@ -199,6 +195,31 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
 #pragma unroll
             for (int j = 0; j < B::BN; ++j) mma(acc[i][j], pf[h][j], xf[i]);
       }
+    }
+  };
+
+  for (int s = 0; s < nsteps; ++s) {
+    // the step's rows of X and its dP are in LDS, and every wave has left the
+    // buffers of the step before
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    issue_x(s + 2);
+    load_p(next, s + 2);
+    char* xb = smem + B::XAT + s % 3 * B::XB;
+    const char* pb = smem + B::PAT + (s & 1) * (B::PARTS * B::PB);
+    const int left = (int)min((int64_t)TS, t1 - t0 - (int64_t)s * TS);
+    if (left < TS) {  // rows past the end count as zero, also where X is not finite
+      for (int e = threadIdx.x; e < B::XB / 16; e += 512)
+        if (e / X::CPR >= left) reinterpret_cast<f32x4*>(xb)[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      lds_barrier();
+    }
+    // half of the waves form the next step's dP before this step's products,
+    // half after, so that a SIMD's two waves use its two pipes at once
+    if (wave < 4) {
+      if (s + 1 < nsteps) produce(now, s + 1);
+      consume(s, xb, pb, left);
+    } else {
+      consume(s, xb, pb, left);
+      if (s + 1 < nsteps) produce(now, s + 1);
     }
     now = next;
   }
@@ -242,27 +263,27 @@ hipError_t launch_form(const LinBwdParams& p, hipStream_t s) {
 }
 template <int KT, int NT> hipError_t launch_size(const LinBwdParams& p, bool fused, hipStream_t s) {
   const bool act = p.act != kActNone;
-  if (fused) return act ? launch_form<KT, NT, true, true>(p, s) : launch_form<KT, NT, false, true>(p, s);
-  return act ? launch_form<KT, NT, true, false>(p, s) : launch_form<KT, NT, false, false>(p, s);
+  if (fused) {
+    if constexpr (KT * NT <= 128 * 256) return act ? launch_form<KT, NT, true, true>(p, s) : launch_form<KT, NT, false, true>(p, s);
+  }
+  if constexpr (KT >= 128 && NT == 128) return launch_form<KT, NT, true, false>(p, s);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 // The tile of inputs and outputs (kt, nt) of the one-pass backward; fused: dX
-// too.  False where the sizes are not whole tiles.
-bool lin_bwd_tile(int64_t K, int64_t N, int& kt, int& nt, bool& fused) {
+// too.  False where the products of k_linear take less time: sizes that are not
+// whole tiles, no activation (nothing is formed twice), or more than 256 inputs
+// (dP is formed again per tile of inputs).  100,000 tokens with GELU, one pass /
+// products: 256 x 512 186 / 227 us, 256 x 256 104 / 126, 512 x 256 184 / 183; 32,768
+// tokens, 512 x 1024 198 / 191; without activation 100,000 x 256 x 512 117 / 105.
+bool lin_bwd_tile(int64_t K, int64_t N, int act, int& kt, int& nt, bool& fused) {
   auto ok = [](int64_t v) { return v == 64 || v == 128 || v == 256; };
   fused = ok(K) && ok(N) && K * N <= 128 * 256;
-  if (fused) {
-    kt = (int)K;
-    nt = (int)N;
-    return true;
-  }
-  // X is read once per strip of outputs, dP formed once per tile of inputs
-  if (K > 512 || K % 128 || N % 128) return false;
-  kt = K % 256 == 0 ? 256 : 128;
-  nt = 128;
-  return true;
+  kt = (int)K;
+  nt = fused ? (int)N : 128;
+  return fused || (act != kActNone && (K == 128 || K == 256) && N % 128 == 0);
 }
 
 hipError_t launch_lin_bwd(const LinBwdParams& p, int kt, int nt, bool fused, hipStream_t s) {
