@@ -176,9 +176,9 @@ LinBwdWs lin_bwd_ws(void* base, int dtype, int act, int64_t rows, int64_t K, int
   }
   w.chunk = std::max<int64_t>(64, cdiv(rows, 512));
   w.pass = dtype == FLAREPP_BF16 && rows >= kLinBwdFrom && lin_bwd_tile(K, N, act, w.kt, w.nt, w.fused);
-  if (w.pass) {  // a workgroup per CU, of 256 tokens at least (its partial sums are as many bytes)
+  if (w.pass) {  // a workgroup per CU, of two steps at least
     const int64_t tiles = (K / w.kt) * (N / w.nt);
-    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, rows / 256));
+    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, rows / 64));
     w.chunk = cdiv(cdiv(rows, groups), 32) * 32;
   }
   w.nchunks = (int)cdiv(rows, w.chunk);

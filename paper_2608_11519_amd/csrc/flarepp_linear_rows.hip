@@ -13,8 +13,12 @@ namespace {
 // follows the weights' copy.
 // STEPS: K is whole steps of 16 (else rows are read by single elements).
 // WHOLE: Q is whole blocks of 32.
+// Waves per SIMD: four for the narrowest strip (500,000 x 64 -> 4 25 -> 21 us), two
+// for the others, whose loads ahead are worth more than the waves (1,048,576 x
+// 64 -> 64 101 us, 115 with four; 200,000 x 512 -> 128 82, 109).
+constexpr int rows_waves(int nb) { return nb == 32 ? 4 : 2; }
 template <typename T, bool RT, int NB, bool STEPS, bool WHOLE>
-__global__ __launch_bounds__(512) void k_linear_rows(LinGemmParams p) {
+__global__ __launch_bounds__(512, rows_waves(NB)) void k_linear_rows(LinGemmParams p) {
   using F = typename Frag<T>::type;
   using R = Tile<T, RT, NB>;
   constexpr int EPC = R::EPC, BK = R::BK, NQ = NB / 32, KPB = BK / 16;  // steps of a buffer of BK
@@ -145,7 +149,8 @@ template <typename T, bool RT, int NB, bool STEPS, bool WHOLE>
 hipError_t launch_strip(const LinGemmParams& p, hipStream_t s) {
   const int64_t tiles = (p.P + 31) / 32, strips = (p.Q + NB - 1) / NB;
   const size_t lds = lin_rows_lds(sizeof(T), NB, p.K);
-  const int64_t groups = std::min<int64_t>((tiles + 7) / 8, std::max<int64_t>(1, 256 / strips));
+  const int64_t per_cu = rows_waves(NB) == 4 && 2 * lds <= 160 * 1024 ? 2 : 1;
+  const int64_t groups = std::min<int64_t>((tiles + 7) / 8, std::max<int64_t>(1, 256 * per_cu / strips));
   auto* kernel = k_linear_rows<T, RT, NB, STEPS, WHOLE>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
   if (e != hipSuccess) return e;
@@ -179,15 +184,17 @@ size_t lin_rows_lds(int elem_bytes, int strip, int64_t K) {
 
 // The strip for a product, or 0 where another kernel has to do: rows of L that
 // are whole steps, or short; outputs that are whole blocks, or (forward) few;
-// weights that fit; and L read at most twice.
+// weights that fit; and L read at most twice.  Rows / tiles: 131,072 x 256 -> 128
+// 29 / 37 us, 100,000 x 256 -> 512 (two strips) 78 / 85, 200,000 x 512 -> 128 82 / 101;
+// beyond, 200,000 x 1024 -> 64 114 / 98, 100,000 x 512 -> 256 (two strips) 63 / 56.
 int lin_rows_strip(int prod, int elem_bytes, int64_t Q, int64_t K) {
   const bool whole = Q % 32 == 0, steps = K % 16 == 0;
-  if (prod == kLinWeight || K > 4096 || (!steps && (K > 32 || !whole)) || (!whole && (prod != kLinForward || Q > 64))) return 0;
+  if (prod == kLinWeight || K > 512 || (!steps && (K > 32 || !whole)) || (!whole && (prod != kLinForward || Q > 64))) return 0;
   const int widest = elem_bytes == 2 ? 256 : 64;
   int strip = 32;
   while (strip < widest && strip < Q) strip *= 2;
   while (strip > 32 && lin_rows_lds(elem_bytes, strip, K) > kLinRowsLds) strip /= 2;
-  return lin_rows_lds(elem_bytes, strip, K) <= kLinRowsLds && (Q + strip - 1) / strip <= 2 ? strip : 0;
+  return lin_rows_lds(elem_bytes, strip, K) <= kLinRowsLds && (Q + strip - 1) / strip <= (K < 512 ? 2 : 1) ? strip : 0;
 }
 
 template <typename T>
