@@ -416,7 +416,8 @@ FLAREPP_API int flarepp_mixer_stage(int stage, int dtype, int64_t B, int64_t N, 
  * T <= 2^30, K and N <= 65536 of any parity, T * max(K, N) <= 2^40 (UNSUPPORTED
  * beyond).  `out` may be `residual` itself; no other output may overlap an
  * input or another output.  Workspace: flarepp_linear_workspace_bytes(...)
- * bytes (0 for an invalid shape).
+ * bytes (0 for an invalid shape; 256, the least, where the call uses none: ws
+ * may then be NULL).
  * ------------------------------------------------------------------------- */
 #define FLAREPP_ACT_NONE 0
 #define FLAREPP_ACT_RELU 1
@@ -460,7 +461,8 @@ FLAREPP_API int flarepp_linear_backward(int dtype, int act, int64_t T, int64_t K
  * symbol, and the sums, fp32, run over ascending positions in an order that
  * depends on the ids alone.  Workspace:
  * flarepp_embedding_backward_workspace_bytes(...) bytes (0 for an invalid
- * shape).  No output may overlap an input.
+ * shape; 256, the least, where the call uses none: ws may then be NULL).  No
+ * output may overlap an input.
  * ------------------------------------------------------------------------- */
 FLAREPP_API int flarepp_embedding_forward(int dtype, int64_t T, int64_t V, int64_t C, const int64_t* ids,
                                           const void* table, float scale, void* out, void* stream);

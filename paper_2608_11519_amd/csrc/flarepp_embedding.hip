@@ -69,28 +69,32 @@ __device__ __forceinline__ uint32_t embed_key(const EmbedGradParams& p, int pass
   return id < 0 || id >= p.V ? (uint32_t)p.V : (uint32_t)id;
 }
 
-// counts[digit][workgroup]; the first pass also clears the table's gradient
-__global__ __launch_bounds__(256) void k_embed_count(EmbedGradParams p, int pass, int nb) {
-  __shared__ int hist[1024];
-  const int bins = 1 << p.bits, shift = pass * p.bits;
-  for (int b = threadIdx.x; b < bins; b += 256) hist[b] = 0;
-  __syncthreads();
-  const int64_t i0 = (int64_t)blockIdx.x * kEmbedTile;
-#pragma unroll
-  for (int u = 0; u < kEmbedTile / 256; ++u) {
-    const int64_t i = i0 + u * 256 + threadIdx.x;
-    if (i < p.T) atomicAdd(&hist[embed_key(p, pass, i) >> shift & (bins - 1)], 1);
-  }
-  __syncthreads();
-  for (int b = threadIdx.x; b < bins; b += 256) p.counts[(int64_t)b * nb + blockIdx.x] = hist[b];
-}
-
-__global__ __launch_bounds__(256) void k_embed_clear(float* p, int64_t n) {
+__device__ __forceinline__ void clear_slice(float* p, int64_t n) {
   const int64_t stride = (int64_t)gridDim.x * 256;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n / 4; i += stride)
     reinterpret_cast<f32x4*>(p)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int64_t tail = n / 4 * 4 + threadIdx.x;
   if (blockIdx.x == 0 && tail < n) p[tail] = 0.f;
+}
+__global__ __launch_bounds__(256) void k_embed_clear(float* p, int64_t n) { clear_slice(p, n); }
+
+// counts[digit][workgroup] of tiles of TILE positions; the first pass also
+// clears the table's gradient
+template <int TILE>
+__global__ __launch_bounds__(256) void k_embed_count(EmbedGradParams p, int pass, int nb) {
+  __shared__ int hist[1024];
+  const int bins = 1 << p.bits, shift = pass * p.bits;
+  for (int b = threadIdx.x; b < bins; b += 256) hist[b] = 0;
+  __syncthreads();
+  const int64_t i0 = (int64_t)blockIdx.x * TILE;
+#pragma unroll
+  for (int u = 0; u < TILE / 256; ++u) {
+    const int64_t i = i0 + u * 256 + threadIdx.x;
+    if (i < p.T) atomicAdd(&hist[embed_key(p, pass, i) >> shift & (bins - 1)], 1);
+  }
+  if (pass == 0) clear_slice(p.dtable, p.V * p.C);
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += 256) p.counts[(int64_t)b * nb + blockIdx.x] = hist[b];
 }
 
 // exclusive sums over the workgroups of a digit, one wave per digit
@@ -114,12 +118,13 @@ __global__ __launch_bounds__(64) void k_embed_scan(EmbedGradParams p, int nb) {
 
 // keys and positions to their places: each wave ranks a run of its
 // workgroup's tile, 64 positions at a time
+template <int TILE>
 __global__ __launch_bounds__(256) void k_embed_scatter(EmbedGradParams p, int pass, int nb) {
   __shared__ int place[4][1024];
   __shared__ int sums[256];
   const int bins = 1 << p.bits, shift = pass * p.bits, lane = lane_id(), wave = wave_id();
-  constexpr int PER = kEmbedTile / 4;  // positions of a wave
-  const int64_t i0 = (int64_t)blockIdx.x * kEmbedTile + wave * PER;
+  constexpr int PER = TILE / 4;  // positions of a wave
+  const int64_t i0 = (int64_t)blockIdx.x * TILE + wave * PER;
   uint32_t key[PER / 64];
 #pragma unroll
   for (int u = 0; u < PER / 64; ++u) {
@@ -237,18 +242,19 @@ __global__ __launch_bounds__(256) void k_embed_runs(EmbedGradParams p, int cl) {
   flush(i1 < p.T && key[i1] == cur);
 }
 
+constexpr int kJoin = 512;
 // Rows whose runs cross chunks: the workgroup of the chunk in which a run
-// begins sums its parts, 1024 / 2^cl groups of lanes taking every so many
+// begins sums its parts, kJoin / 2^cl groups of lanes taking every so many
 // chunks, and then the groups' sums in order.
 template <int VEC>
-__global__ __launch_bounds__(1024) void k_embed_join(EmbedGradParams p, int cl) {
-  __shared__ float sums[1024 * VEC];
+__global__ __launch_bounds__(kJoin) void k_embed_join(EmbedGradParams p, int cl) {
+  __shared__ float sums[kJoin * VEC];
   const int64_t chunk = blockIdx.x, i0 = chunk * kEmbedChunk, i1 = i0 + kEmbedChunk;
   if (i1 >= p.T) return;
   const uint32_t* key = p.key[p.passes & 1];
   const uint32_t cur = key[i1 - 1];
   if (cur >= (uint32_t)p.V || key[i1] != cur || (i0 > 0 && key[i0 - 1] == cur)) return;  // whole workgroup
-  const int lc = threadIdx.x & ((1 << cl) - 1), lr = threadIdx.x >> cl, rl = 1024 >> cl;
+  const int lc = threadIdx.x & ((1 << cl) - 1), lr = threadIdx.x >> cl, rl = kJoin >> cl;
   const int64_t col = (((int64_t)blockIdx.y << cl) + lc) * VEC;
   float s[VEC];
 #pragma unroll
@@ -287,13 +293,89 @@ __global__ __launch_bounds__(1024) void k_embed_join(EmbedGradParams p, int cl) 
   }
 }
 
+// Few positions: the workgroup of a symbol's first position lists all of its
+// positions in order and sums their rows, groups of 2^cl lanes taking every so
+// many of them, and then the groups' sums in order.
+template <typename T, int VEC>
+__global__ __launch_bounds__(256) void k_embed_few(EmbedGradParams p, int cl) {
+  constexpr int PER = kEmbedFew / 256;  // positions of a thread, consecutive
+  __shared__ int list[kEmbedFew];
+  __shared__ int counts[5];
+  __shared__ float sums[256 * VEC];
+  const int t = blockIdx.x, n = (int)p.T, lane = lane_id(), wave = wave_id();
+  const int64_t id = p.ids[t];
+  if (id < 0 || id >= p.V) return;  // whole workgroup
+  bool same[PER], earlier = false;
+  int mine = 0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = threadIdx.x * PER + j;
+    same[j] = i < n && p.ids[i] == id;
+    earlier |= same[j] && i < t;
+    mine += same[j];
+  }
+  if (__syncthreads_or(earlier)) return;
+  // places: positions before this thread's, over the wave and the waves before
+  int before = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int o = __shfl_up(before, d);
+    if (lane >= d) before += o;
+  }
+  if (lane == 63) counts[wave] = before;
+  __syncthreads();
+  int total = 0, base = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) base += counts[w];
+    total += counts[w];
+  }
+  base += before - mine;
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+    if (same[j]) list[base++] = threadIdx.x * PER + j;
+  __syncthreads();
+  const int lc = threadIdx.x & ((1 << cl) - 1), lr = threadIdx.x >> cl, rl = 256 >> cl;
+  const int64_t col = (((int64_t)blockIdx.y << cl) + lc) * VEC;
+  float s[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+  if (col < p.C) {
+    constexpr int AHEAD = 4;
+    for (int q = lr; q < total; q += AHEAD * rl) {
+      float v[AHEAD][VEC];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        load_n<T, VEC>(static_cast<const T*>(p.dout) + (int64_t)list[min(q + u * rl, total - 1)] * p.C + col, v[u]);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (q + u * rl < total)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) s[e] += v[u][e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sums[threadIdx.x * VEC + e] = s[e];
+  for (int h = rl / 2; h > 0; h /= 2) {
+    __syncthreads();
+    if (lr < h)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sums[threadIdx.x * VEC + e] += sums[(threadIdx.x + (h << cl)) * VEC + e];
+  }
+  if (lr == 0 && col < p.C) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) s[e] = sums[threadIdx.x * VEC + e] * p.scale;
+    store_n<float, VEC>(p.dtable + id * p.C + col, s);
+  }
+}
+
 template <typename T, int VEC>
 void embed_sums(const EmbedGradParams& p, hipStream_t s) {
   const int64_t lanes = (p.C + VEC - 1) / VEC, chunks = (p.T + kEmbedChunk - 1) / kEmbedChunk;
   const int cl = pow2_log2(lanes, 6);
   const unsigned strips = (unsigned)((lanes + (1 << cl) - 1) >> cl), per = 256u >> cl;
   k_embed_runs<T, VEC><<<dim3((unsigned)((chunks + per - 1) / per), strips), 256, 0, s>>>(p, cl);
-  if (chunks > 1) k_embed_join<VEC><<<dim3((unsigned)(chunks - 1), strips), 1024, 0, s>>>(p, cl);
+  if (chunks > 1) k_embed_join<VEC><<<dim3((unsigned)(chunks - 1), strips), kJoin, 0, s>>>(p, cl);
 }
 
 }  // namespace
@@ -312,19 +394,36 @@ hipError_t launch_embed(const EmbedParams& p, hipStream_t s) {
 template hipError_t launch_embed<float>(const EmbedParams&, hipStream_t);
 template hipError_t launch_embed<__bf16>(const EmbedParams&, hipStream_t);
 
+template <typename T, int VEC>
+void embed_few(const EmbedGradParams& p, hipStream_t s) {
+  const int64_t lanes = (p.C + VEC - 1) / VEC;
+  const int cl = pow2_log2(lanes, 8);
+  k_embed_few<T, VEC><<<dim3((unsigned)p.T, (unsigned)((lanes + (1 << cl) - 1) >> cl)), 256, 0, s>>>(p, cl);
+}
+template <int TILE> void embed_sort(const EmbedGradParams& p, hipStream_t s) {
+  const int nb = (int)((p.T + TILE - 1) / TILE);
+  for (int pass = 0; pass < p.passes; ++pass) {
+    k_embed_count<TILE><<<dim3(nb), 256, 0, s>>>(p, pass, nb);
+    k_embed_scan<<<dim3(1u << p.bits), 64, 0, s>>>(p, nb);
+    k_embed_scatter<TILE><<<dim3(nb), 256, 0, s>>>(p, pass, nb);
+  }
+}
+
 template <typename T>
 hipError_t launch_embed_grad(const EmbedGradParams& p, hipStream_t s) {
-  const int nb = (int)((p.T + kEmbedTile - 1) / kEmbedTile);
-  const int64_t n = p.V * p.C;
-  k_embed_clear<<<dim3((unsigned)std::min<int64_t>(2048, (n + 1023) / 1024)), 256, 0, s>>>(p.dtable, n);
-  for (int pass = 0; pass < p.passes; ++pass) {
-    k_embed_count<<<dim3(nb), 256, 0, s>>>(p, pass, nb);
-    k_embed_scan<<<dim3(1u << p.bits), 64, 0, s>>>(p, nb);
-    k_embed_scatter<<<dim3(nb), 256, 0, s>>>(p, pass, nb);
-  }
   // 16 bytes of a row of dOut per lane; the sums are stored as whole vectors too
   constexpr int V = 16 / (int)sizeof(T);
-  if (p.C % V == 0) embed_sums<T, V>(p, s);
+  const bool whole = p.C % V == 0;
+  if (p.T <= kEmbedFew) {
+    const int64_t n = p.V * p.C;
+    k_embed_clear<<<dim3((unsigned)std::min<int64_t>(2048, (n + 1023) / 1024)), 256, 0, s>>>(p.dtable, n);
+    if (whole) embed_few<T, V>(p, s);
+    else embed_few<T, 1>(p, s);
+    return hipGetLastError();
+  }
+  if (embed_tile(p.T) == kEmbedTileSmall) embed_sort<kEmbedTileSmall>(p, s);
+  else embed_sort<kEmbedTile>(p, s);
+  if (whole) embed_sums<T, V>(p, s);
   else embed_sums<T, 1>(p, s);
   return hipGetLastError();
 }

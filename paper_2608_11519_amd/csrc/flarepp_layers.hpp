@@ -98,7 +98,11 @@ struct EmbedGradParams {
   float* part;  // [chunks][2][C]: the sums of runs that cross a chunk's start, end
   int passes, bits;
 };
-constexpr int kEmbedTile = 2048;  // positions of a workgroup of the sort
+constexpr int kEmbedFew = 2048;   // positions up to which no sort is needed
+// positions of a workgroup of the sort: small ones until they would make more
+// workgroups than the card takes at once
+constexpr int kEmbedTileSmall = 512, kEmbedTile = 2048;
+constexpr int embed_tile(int64_t T) { return T <= (1 << 18) ? kEmbedTileSmall : kEmbedTile; }
 constexpr int kEmbedChunk = 64;   // sorted positions summed by one group of lanes
 template <typename T> hipError_t launch_embed_grad(const EmbedGradParams&, hipStream_t);
 

@@ -174,7 +174,8 @@ LinBwdWs lin_bwd_ws(void* base, int dtype, int act, int64_t rows, int64_t K, int
     w.dp = cv.take(bs * rows * N);
     if (dtype == FLAREPP_BF16) w.dp_lo = cv.take(bs * rows * N);
   }
-  w.chunk = std::max<int64_t>(64, cdiv(rows, 512));
+  // (few rows: one chunk, and no sum of partials)
+  w.chunk = rows <= 128 ? rows : std::max<int64_t>(64, cdiv(rows, 512));
   w.pass = dtype == FLAREPP_BF16 && rows >= kLinBwdFrom && lin_bwd_tile(K, N, act, w.kt, w.nt, w.fused);
   if (w.pass) {  // a workgroup per CU, of two steps at least
     const int64_t tiles = (K / w.kt) * (N / w.nt);
@@ -226,7 +227,7 @@ int run_linear_backward(int dtype, int act, int64_t rows, int64_t K, int64_t N, 
       p.dp_lo = dW ? w.dp_lo : nullptr;
       dp = w.dp;
     }
-    p.part = dbias ? w.bias_part : nullptr;
+    p.part = w.nchunks == 1 ? dbias : dbias ? w.bias_part : nullptr;
     p.part_ld = w.bias_ld; p.nchunks = w.nchunks; p.chunk = w.chunk;
     HIPTRY(launch_lin_slope<T>(p, s));
   }
@@ -245,7 +246,7 @@ int run_linear_backward(int dtype, int act, int64_t rows, int64_t K, int64_t N, 
     else p.part = dW;
     HIPTRY(launch_lin_gemm<T>(p, kLinWeight, w.dw.tile, w.dw.direct, s));
   }
-  if (dbias) sums.job[sums.njobs++] = {w.bias_part, w.bias_ld, N, w.nchunks, dbias};
+  if (dbias && w.nchunks > 1) sums.job[sums.njobs++] = {w.bias_part, w.bias_ld, N, w.nchunks, dbias};
   if (sums.njobs) HIPTRY(launch_lin_sum(sums, s));
   return api_ok();
 }
@@ -265,7 +266,8 @@ size_t embed_ws(EmbedGradParams& p, void* base) {
   while ((int64_t(1) << bits) <= p.V) ++bits;  // symbols 0 .. V - 1, and V for padding
   p.passes = (bits + 9) / 10;
   p.bits = (bits + p.passes - 1) / p.passes;
-  const int64_t nb = cdiv(p.T, kEmbedTile), chunks = cdiv(p.T, kEmbedChunk);
+  if (p.T <= kEmbedFew) return 0;
+  const int64_t nb = cdiv(p.T, embed_tile(p.T)), chunks = cdiv(p.T, kEmbedChunk);
   Carver cv{static_cast<char*>(base)};
   for (int i = 0; i < 2; ++i) {
     p.key[i] = static_cast<uint32_t*>(cv.take(4 * p.T));
@@ -390,7 +392,7 @@ int flarepp_linear_forward(int dtype, int act, int64_t T, int64_t K, int64_t N, 
   TRY(check_ptr(pre, "pre", true));
   if (out == X || out == W || pre == X || pre == W || pre == out || (pre && pre == residual))
     return fail(FLAREPP_ERR_INVALID_ARG, "out and pre must not be X, W or each other, nor pre the residual");
-  TRY(check_ws(ws, ws_bytes, flarepp_linear_workspace_bytes(dtype, T, K, N)));
+  TRY(check_ws(ws, ws_bytes, lin_plan(kLinForward, dtype == FLAREPP_F32 ? 4 : 2, T, N, K).part_bytes));
   hipStream_t s = static_cast<hipStream_t>(stream);
   return dtype == FLAREPP_F32 ? run_linear<float>(act, T, K, N, X, W, bias, residual, out, pre, ws, s)
                               : run_linear<__bf16>(act, T, K, N, X, W, bias, residual, out, pre, ws, s);
@@ -437,7 +439,7 @@ size_t flarepp_embedding_backward_workspace_bytes(int64_t T, int64_t V, int64_t 
   if (check_embedding_shape(FLAREPP_F32, T, V, C) != FLAREPP_OK) return 0;
   EmbedGradParams p{};
   p.T = T; p.V = V; p.C = C;
-  return embed_ws(p, nullptr);
+  return std::max<size_t>(256, embed_ws(p, nullptr));
 }
 
 int flarepp_embedding_backward(int dtype, int64_t T, int64_t V, int64_t C, const int64_t* ids, const void* dOut, float scale,
@@ -447,10 +449,9 @@ int flarepp_embedding_backward(int dtype, int64_t T, int64_t V, int64_t C, const
   TRY(check_ptr(dOut, "dOut"));
   TRY(check_ptr(dTable, "dTable"));
   if ((const void*)dTable == dOut) return fail(FLAREPP_ERR_INVALID_ARG, "dTable must not be dOut");
-  TRY(check_ws(ws, ws_bytes, flarepp_embedding_backward_workspace_bytes(T, V, C)));
   EmbedGradParams p{};
   p.ids = ids; p.dout = dOut; p.T = T; p.V = V; p.C = C; p.scale = scale; p.dtable = dTable;
-  embed_ws(p, ws);
+  TRY(check_ws(ws, ws_bytes, embed_ws(p, ws)));
   hipStream_t s = static_cast<hipStream_t>(stream);
   HIPTRY(dtype == FLAREPP_F32 ? launch_embed_grad<float>(p, s) : launch_embed_grad<__bf16>(p, s));
   return api_ok();

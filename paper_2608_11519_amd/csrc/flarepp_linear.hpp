@@ -124,7 +124,7 @@ template <typename T, bool TR, int ROWS, int KB = 128> struct Tile {
 };
 
 // One 16-byte chunk of an operand with `rows` rows and reduction length kend,
-// zeros outside; by elements where rows of the array are not whole chunks.
+// zeros outside; `whole`: rows of the array are whole chunks.
 template <typename T, bool TR>
 __device__ __forceinline__ f32x4 guarded_chunk(const T* src, int64_t ld, int64_t rows, int64_t kend, int64_t row, int64_t k,
                                                bool whole) {
@@ -136,6 +136,10 @@ __device__ __forceinline__ f32x4 guarded_chunk(const T* src, int64_t ld, int64_t
   const T* s = src + sr * ld + sc;
   if (whole) {
     if (sc < ce) v = *reinterpret_cast<const f32x4*>(s);
+    return v;
+  }
+  if (sc + EPC <= ce) {
+    __builtin_memcpy(&v, s, 16);  // at any address
     return v;
   }
   T e[EPC];
@@ -152,9 +156,17 @@ __device__ __forceinline__ void store_part(T* out, int64_t Q, int64_t row, int64
     store4(out + row * Q + q, v[0], v[1], v[2], v[3]);
     return;
   }
+  T w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = from_f32<T>(v[e]);
+  T* at = out + row * Q + q;
+  if (q + 4 <= Q) {
+    __builtin_memcpy(at, w, sizeof(w));  // at any address
+    return;
+  }
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (q + e < Q) out[row * Q + q + e] = from_f32<T>(v[e]);
+    if (q + e < Q) at[e] = w[e];
 }
 // Four consecutive values from q on, zeros past the end of the row
 template <typename T>
@@ -163,6 +175,11 @@ __device__ __forceinline__ void read_part(const T* src, int64_t at, int64_t q, i
     const auto x = load_half(src + at + q);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = to_f32(x[e]);
+  } else if (q + 4 <= Q) {
+    T w[4];
+    __builtin_memcpy(w, src + at + q, sizeof(w));  // at any address
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = to_f32(w[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = q + e < Q ? to_f32(src[at + q + e]) : 0.f;

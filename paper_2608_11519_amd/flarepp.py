@@ -683,9 +683,14 @@ def flarepp_block_backward(X, gamma, beta, Wk, Wv, Wkt, Wvt, Wo, seeds, dO, *, H
 # operators around the mixer: linear layer, embedding, optimiser step
 # ---------------------------------------------------------------------------
 
+_NO_CONTEXT = contextlib.nullcontext()
+
+
 def _on_device(device: torch.device):
     """Context in which ``device`` is the current one, as launches need."""
-    return torch.cuda.device(device) if device.type == "cuda" else contextlib.nullcontext()
+    if device.type != "cuda" or device.index == torch.cuda.current_device():
+        return _NO_CONTEXT
+    return torch.cuda.device(device)
 
 
 def _layer(X, W):
@@ -720,6 +725,16 @@ def _check_ws(ws, device) -> None:
         raise ValueError(f"ws is on {ws.device}, expected {device}")
 
 
+def _optional_workspace(nbytes: int, device, ws):
+    """As _workspace, for the entry points whose least size (256 bytes) says
+    that the call needs none."""
+    return ws if ws is None and nbytes <= 256 else _workspace(nbytes, device, ws)
+
+
+def _ws_args(w):
+    return (None, 0) if w is None else (_ptr(w), w.numel())
+
+
 def flarepp_linear_workspace_bytes(dtype: int, T: int, K: int, N: int) -> int:
     return int(load().flarepp_linear_workspace_bytes(dtype, T, K, N))
 
@@ -743,10 +758,10 @@ def flarepp_linear_forward(X: torch.Tensor, W: torch.Tensor, bias: Optional[torc
     dt = _dtype_code(X)
     O = out if out is not None else torch.empty(shape, dtype=X.dtype, device=X.device)
     pre = torch.empty(shape, dtype=X.dtype, device=X.device) if keep_pre else None
-    w = _workspace(flarepp_linear_workspace_bytes(dt, T, K, N), X.device, ws)
+    w = _optional_workspace(lib.flarepp_linear_workspace_bytes(dt, T, K, N), X.device, ws)
     with _on_device(X.device):
         rc = lib.flarepp_linear_forward(dt, act, T, K, N, _ptr(X), _ptr(W), _ptr(bias), _ptr(residual), _ptr(O), _ptr(pre),
-                                        _ptr(w), w.numel(), _stream(X.device))
+                                        *_ws_args(w), _stream(X.device))
     _check(rc)
     return (O, pre) if keep_pre else O
 
@@ -781,10 +796,10 @@ def flarepp_linear_backward(X: torch.Tensor, W: torch.Tensor, dOut: torch.Tensor
         g = {k: torch.empty(shape, dtype=dtype, device=X.device) for (k, (shape, dtype)), want
              in zip(forms.items(), (want_dX, want_dW, want_dbias)) if want}
     dt = _dtype_code(X)
-    w = _workspace(flarepp_linear_backward_workspace_bytes(dt, act, T, K, N), X.device, ws)
+    w = _workspace(lib.flarepp_linear_backward_workspace_bytes(dt, act, T, K, N), X.device, ws)
     with _on_device(X.device):
         rc = lib.flarepp_linear_backward(dt, act, T, K, N, _ptr(X), _ptr(W), _ptr(pre), _ptr(dOut),
-                                         *[_ptr(g.get(k)) for k in forms], _ptr(w), w.numel(), _stream(X.device))
+                                         *[_ptr(g.get(k)) for k in forms], *_ws_args(w), _stream(X.device))
     _check(rc)
     return g
 
@@ -848,9 +863,9 @@ def flarepp_embedding_backward(ids: torch.Tensor, dOut: torch.Tensor, *, V: int,
     if not need:
         _check(ERR_INVALID_ARG if min(T, V, C) < 1 else ERR_UNSUPPORTED)
     g = out if out is not None else torch.empty((V, C), dtype=torch.float32, device=ids.device)
-    w = _workspace(need, ids.device, ws)
+    w = _optional_workspace(need, ids.device, ws)
     with _on_device(ids.device):
-        rc = lib.flarepp_embedding_backward(dt, T, V, C, _ptr(ids), _ptr(dOut), float(scale), _ptr(g), _ptr(w), w.numel(),
+        rc = lib.flarepp_embedding_backward(dt, T, V, C, _ptr(ids), _ptr(dOut), float(scale), _ptr(g), *_ws_args(w),
                                             _stream(ids.device))
     _check(rc)
     return g

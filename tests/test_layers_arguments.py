@@ -20,7 +20,7 @@ def _lib():
     fp.load()
 
 
-def _forward(dtype=fp.BF16, act=fp.ACT_GELU, T=100, K=64, N=32, ptrs=None, ws=_P[15], nbytes=1 << 30):
+def _forward(dtype=fp.BF16, act=fp.ACT_GELU, T=100, K=1024, N=32, ptrs=None, ws=_P[15], nbytes=1 << 30):
     return fp.load().flarepp_linear_forward(dtype, act, T, K, N, *(ptrs or _P[:6]), ws, nbytes, None)
 
 
@@ -73,6 +73,10 @@ def test_linear_workspaces():
     # the activation's gradient (two parts with bf16) and the bias sums
     assert fp.flarepp_linear_backward_workspace_bytes(fp.BF16, fp.ACT_GELU, T, K, N) >= 4 * T * N
     assert fp.flarepp_linear_backward_workspace_bytes(fp.F32, fp.ACT_GELU, T, K, N) >= 4 * T * N
+    # no workspace where the reduction is not split
+    assert fp.flarepp_linear_workspace_bytes(fp.BF16, 100, 64, 32) == 256
+    assert fp.flarepp_linear_workspace_bytes(fp.BF16, 100, 1024, 32) > 256
+    assert fp.flarepp_embedding_backward_workspace_bytes(100, 5, 8) == 256
     # what is summed per split does not grow with the tokens
     a, b = (fp.flarepp_linear_backward_workspace_bytes(fp.BF16, fp.ACT_NONE, t, K, N) for t in (1 << 18, 1 << 24))
     assert b <= 1.1 * a
@@ -94,7 +98,8 @@ def test_embedding_refuses():
                 p[i] = bad
                 assert f(p=p) == fp.ERR_INVALID_ARG
         assert f(p=[_P[0], _P[1], _P[1]]) == fp.ERR_INVALID_ARG
-    assert bwd(ws=None) == fp.ERR_WORKSPACE and bwd(n=64) == fp.ERR_WORKSPACE
+    many = dict(T=10000, V=5, C=8)
+    assert bwd(ws=None, **many) == fp.ERR_WORKSPACE and bwd(n=64, **many) == fp.ERR_WORKSPACE
     assert fp.flarepp_embedding_backward_workspace_bytes(0, 5, 8) == 0
 
 
