@@ -15,24 +15,40 @@ int pow2_log2(int64_t n, int most) {  // of the smallest power of two >= n, at m
   return l;
 }
 
-// N values of T as floats, and back
-template <typename T, int N> constexpr int align_n() { return N * (int)sizeof(T) < 16 ? N * (int)sizeof(T) : 16; }
-template <typename T, int N> __device__ __forceinline__ void load_n(const T* p, float (&v)[N]) {
+// N values of T from column col of a row of C as floats, and back.  WHOLE: rows
+// are whole vectors of 16 bytes; else the vectors lie at any address and the
+// row's last one is cut.
+template <typename T, int N, bool WHOLE> __device__ __forceinline__ void load_n(const T* row, int64_t col, int64_t C, float (&v)[N]) {
   T e[N];
-  __builtin_memcpy(e, __builtin_assume_aligned(p, align_n<T, N>()), N * sizeof(T));
+  if constexpr (WHOLE) {
+    __builtin_memcpy(e, __builtin_assume_aligned(row + col, N * sizeof(T) < 16 ? N * sizeof(T) : 16), N * sizeof(T));
+  } else if (col + N <= C) {
+    __builtin_memcpy(e, row + col, N * sizeof(T));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) e[i] = col + i < C ? row[col + i] : from_f32<T>(0.f);
+  }
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = to_f32(e[i]);
 }
-template <typename T, int N> __device__ __forceinline__ void store_n(T* p, const float (&v)[N]) {
+template <typename T, int N, bool WHOLE> __device__ __forceinline__ void store_n(T* row, int64_t col, int64_t C, const float (&v)[N]) {
   T e[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) e[i] = from_f32<T>(v[i]);
-  __builtin_memcpy(__builtin_assume_aligned(p, align_n<T, N>()), e, N * sizeof(T));
+  if constexpr (WHOLE) {
+    __builtin_memcpy(__builtin_assume_aligned(row + col, N * sizeof(T) < 16 ? N * sizeof(T) : 16), e, N * sizeof(T));
+  } else if (col + N <= C) {
+    __builtin_memcpy(row + col, e, N * sizeof(T));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (col + i < C) row[col + i] = e[i];
+  }
 }
 
 // out[t] = scale * table[ids[t]]: VEC channels per lane, 2^cl lanes across a
 // row, four rows per lane so that their loads are in flight together.
-template <typename T, int VEC>
+template <typename T, int VEC, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed(EmbedParams p, int cl) {
   constexpr int ROWS = 4;
   const int rl = 256 >> cl, lr = threadIdx.x >> cl;
@@ -45,7 +61,7 @@ __global__ __launch_bounds__(256) void k_embed(EmbedParams p, int cl) {
   for (int r = 0; r < ROWS; ++r) id[r] = t0 + r * rl < p.T ? p.ids[t0 + r * rl] : -1;
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
-    if (id[r] >= 0 && id[r] < p.V) load_n<T, VEC>(static_cast<const T*>(p.table) + id[r] * p.C + col, v[r]);
+    if (id[r] >= 0 && id[r] < p.V) load_n<T, VEC, WHOLE>(static_cast<const T*>(p.table) + id[r] * p.C, col, p.C, v[r]);
     else
 #pragma unroll
       for (int e = 0; e < VEC; ++e) v[r][e] = id[r] < 0 ? 0.f : __builtin_nanf("");
@@ -55,7 +71,7 @@ __global__ __launch_bounds__(256) void k_embed(EmbedParams p, int cl) {
     if (t0 + r * rl >= p.T) continue;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) v[r][e] *= p.scale;
-    store_n<T, VEC>(static_cast<T*>(p.out) + (t0 + r * rl) * p.C + col, v[r]);
+    store_n<T, VEC, WHOLE>(static_cast<T*>(p.out) + (t0 + r * rl) * p.C, col, p.C, v[r]);
   }
 }
 
@@ -192,7 +208,7 @@ __global__ __launch_bounds__(256) void k_embed_scatter(EmbedGradParams p, int pa
 // positions, 2^cl lanes per chunk and strip of columns.  A run inside one
 // chunk is a row of the result; parts of longer runs go to part[chunk][0]
 // (began before the chunk) or [1] (goes on after it).
-template <typename T, int VEC>
+template <typename T, int VEC, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed_runs(EmbedGradParams p, int cl) {
   const int64_t col = (((int64_t)blockIdx.y << cl) + (threadIdx.x & ((1 << cl) - 1))) * VEC;
   const int64_t chunk = ((int64_t)blockIdx.x << (8 - cl)) + (threadIdx.x >> cl);
@@ -208,11 +224,11 @@ __global__ __launch_bounds__(256) void k_embed_runs(EmbedGradParams p, int cl) {
   auto flush = [&](bool tail) __attribute__((always_inline)) {
     if (cur >= (uint32_t)p.V) return;  // padding
     if (head || tail) {
-      store_n<float, VEC>(p.part + (2 * chunk + (head ? 0 : 1)) * p.C + col, s);
+      store_n<float, VEC, WHOLE>(p.part + (2 * chunk + (head ? 0 : 1)) * p.C, col, p.C, s);
     } else {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) s[e] *= p.scale;
-      store_n<float, VEC>(p.dtable + (int64_t)cur * p.C + col, s);
+      store_n<float, VEC, WHOLE>(p.dtable + (int64_t)cur * p.C, col, p.C, s);
     }
   };
   constexpr int AHEAD = 8;
@@ -223,7 +239,7 @@ __global__ __launch_bounds__(256) void k_embed_runs(EmbedGradParams p, int cl) {
     for (int u = 0; u < AHEAD; ++u) {
       const int64_t at = min(i + u, i1 - 1);
       k[u] = key[at];
-      load_n<T, VEC>(static_cast<const T*>(p.dout) + (int64_t)pos[at] * p.C + col, v[u]);
+      load_n<T, VEC, WHOLE>(static_cast<const T*>(p.dout) + (int64_t)pos[at] * p.C, col, p.C, v[u]);
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
@@ -246,7 +262,7 @@ constexpr int kJoin = 512;
 // Rows whose runs cross chunks: the workgroup of the chunk in which a run
 // begins sums its parts, kJoin / 2^cl groups of lanes taking every so many
 // chunks, and then the groups' sums in order.
-template <int VEC>
+template <int VEC, bool WHOLE>
 __global__ __launch_bounds__(kJoin) void k_embed_join(EmbedGradParams p, int cl) {
   __shared__ float sums[kJoin * VEC];
   const int64_t chunk = blockIdx.x, i0 = chunk * kEmbedChunk, i1 = i0 + kEmbedChunk;
@@ -260,7 +276,7 @@ __global__ __launch_bounds__(kJoin) void k_embed_join(EmbedGradParams p, int cl)
 #pragma unroll
   for (int e = 0; e < VEC; ++e) s[e] = 0.f;
   if (col < p.C) {
-    if (lr == 0) load_n<float, VEC>(p.part + (2 * chunk + 1) * p.C + col, s);
+    if (lr == 0) load_n<float, VEC, WHOLE>(p.part + (2 * chunk + 1) * p.C, col, p.C, s);
     constexpr int AHEAD = 4;
     for (int64_t q = chunk + 1 + lr; q * kEmbedChunk < p.T && key[q * kEmbedChunk] == cur; q += AHEAD * rl) {
       float v[AHEAD][VEC];
@@ -269,7 +285,7 @@ __global__ __launch_bounds__(kJoin) void k_embed_join(EmbedGradParams p, int cl)
       for (int u = 0; u < AHEAD; ++u) {
         const int64_t at = q + u * rl;
         in[u] = at * kEmbedChunk < p.T && key[at * kEmbedChunk] == cur;
-        if (in[u]) load_n<float, VEC>(p.part + 2 * at * p.C + col, v[u]);
+        if (in[u]) load_n<float, VEC, WHOLE>(p.part + 2 * at * p.C, col, p.C, v[u]);
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
@@ -289,14 +305,14 @@ __global__ __launch_bounds__(kJoin) void k_embed_join(EmbedGradParams p, int cl)
   if (lr == 0 && col < p.C) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) s[e] = sums[threadIdx.x * VEC + e] * p.scale;
-    store_n<float, VEC>(p.dtable + (int64_t)cur * p.C + col, s);
+    store_n<float, VEC, WHOLE>(p.dtable + (int64_t)cur * p.C, col, p.C, s);
   }
 }
 
 // Few positions: the workgroup of a symbol's first position lists all of its
 // positions in order and sums their rows, groups of 2^cl lanes taking every so
 // many of them, and then the groups' sums in order.
-template <typename T, int VEC>
+template <typename T, int VEC, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed_few(EmbedGradParams p, int cl) {
   constexpr int PER = kEmbedFew / 256;  // positions of a thread, consecutive
   __shared__ int list[kEmbedFew];
@@ -341,12 +357,12 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedGradParams p, int cl) {
 #pragma unroll
   for (int e = 0; e < VEC; ++e) s[e] = 0.f;
   if (col < p.C) {
-    constexpr int AHEAD = 4;
+    constexpr int AHEAD = 8;
     for (int q = lr; q < total; q += AHEAD * rl) {
       float v[AHEAD][VEC];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
-        load_n<T, VEC>(static_cast<const T*>(p.dout) + (int64_t)list[min(q + u * rl, total - 1)] * p.C + col, v[u]);
+        load_n<T, VEC, WHOLE>(static_cast<const T*>(p.dout) + (int64_t)list[min(q + u * rl, total - 1)] * p.C, col, p.C, v[u]);
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
         if (q + u * rl < total)
@@ -365,17 +381,17 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedGradParams p, int cl) {
   if (lr == 0 && col < p.C) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) s[e] = sums[threadIdx.x * VEC + e] * p.scale;
-    store_n<float, VEC>(p.dtable + id * p.C + col, s);
+    store_n<float, VEC, WHOLE>(p.dtable + id * p.C, col, p.C, s);
   }
 }
 
-template <typename T, int VEC>
+template <typename T, int VEC, bool WHOLE>
 void embed_sums(const EmbedGradParams& p, hipStream_t s) {
   const int64_t lanes = (p.C + VEC - 1) / VEC, chunks = (p.T + kEmbedChunk - 1) / kEmbedChunk;
   const int cl = pow2_log2(lanes, 6);
   const unsigned strips = (unsigned)((lanes + (1 << cl) - 1) >> cl), per = 256u >> cl;
-  k_embed_runs<T, VEC><<<dim3((unsigned)((chunks + per - 1) / per), strips), 256, 0, s>>>(p, cl);
-  if (chunks > 1) k_embed_join<VEC><<<dim3((unsigned)(chunks - 1), strips), kJoin, 0, s>>>(p, cl);
+  k_embed_runs<T, VEC, WHOLE><<<dim3((unsigned)((chunks + per - 1) / per), strips), 256, 0, s>>>(p, cl);
+  if (chunks > 1) k_embed_join<VEC, WHOLE><<<dim3((unsigned)(chunks - 1), strips), kJoin, 0, s>>>(p, cl);
 }
 
 }  // namespace
@@ -383,22 +399,22 @@ void embed_sums(const EmbedGradParams& p, hipStream_t s) {
 template <typename T>
 hipError_t launch_embed(const EmbedParams& p, hipStream_t s) {
   constexpr int V = 16 / (int)sizeof(T);
-  const bool whole = p.C % V == 0;
-  const int64_t lanes = whole ? p.C / V : p.C;
+  const int64_t lanes = p.C >= V ? (p.C + V - 1) / V : p.C;
   const int cl = pow2_log2(lanes, 8), rows = 4 * (256 >> cl);
   const dim3 grid((unsigned)((p.T + rows - 1) / rows), (unsigned)((lanes + (1 << cl) - 1) >> cl));
-  if (whole) k_embed<T, V><<<grid, 256, 0, s>>>(p, cl);
-  else k_embed<T, 1><<<grid, 256, 0, s>>>(p, cl);
+  if (p.C % V == 0) k_embed<T, V, true><<<grid, 256, 0, s>>>(p, cl);
+  else if (p.C > V) k_embed<T, V, false><<<grid, 256, 0, s>>>(p, cl);
+  else k_embed<T, 1, true><<<grid, 256, 0, s>>>(p, cl);
   return hipGetLastError();
 }
 template hipError_t launch_embed<float>(const EmbedParams&, hipStream_t);
 template hipError_t launch_embed<__bf16>(const EmbedParams&, hipStream_t);
 
-template <typename T, int VEC>
+template <typename T, int VEC, bool WHOLE>
 void embed_few(const EmbedGradParams& p, hipStream_t s) {
   const int64_t lanes = (p.C + VEC - 1) / VEC;
-  const int cl = pow2_log2(lanes, 8);
-  k_embed_few<T, VEC><<<dim3((unsigned)p.T, (unsigned)((lanes + (1 << cl) - 1) >> cl)), 256, 0, s>>>(p, cl);
+  const int cl = pow2_log2(lanes, 5);  // eight groups at least: one symbol may have every position
+  k_embed_few<T, VEC, WHOLE><<<dim3((unsigned)p.T, (unsigned)((lanes + (1 << cl) - 1) >> cl)), 256, 0, s>>>(p, cl);
 }
 template <int TILE> void embed_sort(const EmbedGradParams& p, hipStream_t s) {
   const int nb = (int)((p.T + TILE - 1) / TILE);
@@ -413,18 +429,20 @@ template <typename T>
 hipError_t launch_embed_grad(const EmbedGradParams& p, hipStream_t s) {
   // 16 bytes of a row of dOut per lane; the sums are stored as whole vectors too
   constexpr int V = 16 / (int)sizeof(T);
-  const bool whole = p.C % V == 0;
+  const bool whole = p.C % V == 0, cut = p.C > V;
   if (p.T <= kEmbedFew) {
     const int64_t n = p.V * p.C;
     k_embed_clear<<<dim3((unsigned)std::min<int64_t>(2048, (n + 1023) / 1024)), 256, 0, s>>>(p.dtable, n);
-    if (whole) embed_few<T, V>(p, s);
-    else embed_few<T, 1>(p, s);
+    if (whole) embed_few<T, V, true>(p, s);
+    else if (cut) embed_few<T, V, false>(p, s);
+    else embed_few<T, 1, true>(p, s);
     return hipGetLastError();
   }
   if (embed_tile(p.T) == kEmbedTileSmall) embed_sort<kEmbedTileSmall>(p, s);
   else embed_sort<kEmbedTile>(p, s);
-  if (whole) embed_sums<T, V>(p, s);
-  else embed_sums<T, 1>(p, s);
+  if (whole) embed_sums<T, V, true>(p, s);
+  else if (cut) embed_sums<T, V, false>(p, s);
+  else embed_sums<T, 1, true>(p, s);
   return hipGetLastError();
 }
 template hipError_t launch_embed_grad<float>(const EmbedGradParams&, hipStream_t);

@@ -245,9 +245,10 @@ __global__ __launch_bounds__(256) void k_linear_finish(LinGemmParams p) {
 }
 
 // ---- dP = dOut * act'(pre) and its column sums --------------------------------------------
-// A workgroup takes a chunk of rows and a strip of columns: VEC (16 bytes) or
-// one column per lane, CL lanes across, 256 / CL rows at a time.
-template <typename T, int VEC, int ACT>
+// A workgroup takes a chunk of rows and a strip of columns: VEC columns per
+// lane, 2^cl lanes across, 256 / 2^cl rows at a time.  WHOLE: rows are whole
+// vectors; else the vectors lie at any address and a row's last one is cut.
+template <typename T, int VEC, int ACT, bool WHOLE>
 __global__ __launch_bounds__(256) void k_linear_slope(LinSlopeParams p, int cl_log2) {
   __shared__ float sums[256 * VEC];
   const int cl = 1 << cl_log2, lc = threadIdx.x & (cl - 1), lr = threadIdx.x >> cl_log2, rl = 256 >> cl_log2;
@@ -255,15 +256,31 @@ __global__ __launch_bounds__(256) void k_linear_slope(LinSlopeParams p, int cl_l
   const int64_t r0 = (int64_t)blockIdx.x * p.chunk, r1 = min(p.T, r0 + p.chunk);
   const T* d = static_cast<const T*>(p.dout);
   const T* a = static_cast<const T*>(p.pre);
+  const bool full = WHOLE || col + VEC <= p.N;
   float s[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+  auto get = [&](const T* src, T (&v)[VEC]) __attribute__((always_inline)) {
+    if (WHOLE) __builtin_memcpy(v, __builtin_assume_aligned(src, VEC * sizeof(T)), VEC * sizeof(T));
+    else if (full) __builtin_memcpy(v, src, VEC * sizeof(T));
+    else
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[e] = col + e < p.N ? src[e] : from_f32<T>(0.f);
+  };
+  auto put = [&](T* dst, const T (&v)[VEC]) __attribute__((always_inline)) {
+    if (WHOLE) __builtin_memcpy(__builtin_assume_aligned(dst, VEC * sizeof(T)), v, VEC * sizeof(T));
+    else if (full) __builtin_memcpy(dst, v, VEC * sizeof(T));
+    else
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (col + e < p.N) dst[e] = v[e];
+  };
   if (col < p.N) {
     for (int64_t r = r0 + lr; r < r1; r += rl) {
       const int64_t at = r * p.N + col;
       T dv[VEC], av[VEC], hi[VEC], lo[VEC];
-      __builtin_memcpy(dv, __builtin_assume_aligned(d + at, VEC * sizeof(T)), VEC * sizeof(T));
-      if (ACT != kActNone) __builtin_memcpy(av, __builtin_assume_aligned(a + at, VEC * sizeof(T)), VEC * sizeof(T));
+      get(d + at, dv);
+      if (ACT != kActNone) get(a + at, av);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         float v = to_f32(dv[e]);
@@ -272,8 +289,8 @@ __global__ __launch_bounds__(256) void k_linear_slope(LinSlopeParams p, int cl_l
         hi[e] = from_f32<T>(v);
         lo[e] = from_f32<T>(v - to_f32(hi[e]));
       }
-      if (p.dp) __builtin_memcpy(__builtin_assume_aligned(static_cast<T*>(p.dp) + at, VEC * sizeof(T)), hi, VEC * sizeof(T));
-      if (p.dp_lo) __builtin_memcpy(__builtin_assume_aligned(static_cast<T*>(p.dp_lo) + at, VEC * sizeof(T)), lo, VEC * sizeof(T));
+      if (p.dp) put(static_cast<T*>(p.dp) + at, hi);
+      if (p.dp_lo) put(static_cast<T*>(p.dp_lo) + at, lo);
     }
   }
   if (!p.part) return;
@@ -285,9 +302,10 @@ __global__ __launch_bounds__(256) void k_linear_slope(LinSlopeParams p, int cl_l
 #pragma unroll
       for (int e = 0; e < VEC; ++e) sums[(lr * cl + lc) * VEC + e] += sums[((lr + h) * cl + lc) * VEC + e];
   }
-  if (lr == 0 && col < p.N)
+  if (lr == 0)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) p.part[blockIdx.x * p.part_ld + col + e] = sums[lc * VEC + e];
+    for (int e = 0; e < VEC; ++e)
+      if (col + e < p.N) p.part[blockIdx.x * p.part_ld + col + e] = sums[lc * VEC + e];
 }
 
 // ---- sums of partials in a fixed order ---------------------------------------------------
@@ -379,14 +397,15 @@ template hipError_t launch_lin_finish<__bf16>(const LinGemmParams&, hipStream_t)
 template <typename T>
 hipError_t launch_lin_slope(const LinSlopeParams& p, hipStream_t s) {
   constexpr int V = 16 / (int)sizeof(T);
-  const int vec = p.N % V == 0 ? V : 1;
+  const int vec = p.N >= V ? V : 1;
   int cl = 0;
   while ((1 << cl) < (vec == 1 ? 256 : 32) && (int64_t)vec << cl < p.N) ++cl;
   const dim3 grid((unsigned)p.nchunks, (unsigned)((p.N + ((int64_t)vec << cl) - 1) / ((int64_t)vec << cl)));
   auto go = [&](auto act) {
     constexpr int A = decltype(act)::value;
-    if (vec == 1) k_linear_slope<T, 1, A><<<grid, 256, 0, s>>>(p, cl);
-    else k_linear_slope<T, V, A><<<grid, 256, 0, s>>>(p, cl);
+    if (vec == 1) k_linear_slope<T, 1, A, true><<<grid, 256, 0, s>>>(p, cl);
+    else if (p.N % V == 0) k_linear_slope<T, V, A, true><<<grid, 256, 0, s>>>(p, cl);
+    else k_linear_slope<T, V, A, false><<<grid, 256, 0, s>>>(p, cl);
   };
   if (p.act == kActGelu) go(ActC<kActGelu>{});
   else if (p.act == kActSilu) go(ActC<kActSilu>{});

@@ -36,7 +36,7 @@ def _ids(kind, T, V, seed=0):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,V,C", [(1, 1, 1), (1, 300, 128), (7, 3, 5), (1000, 256, 128), (333, 5000, 130), (50, 9, 2100),
-                                   (4097, 77, 64)])
+                                   (4097, 77, 64), (90, 30, 289), (70, 30, 11)])
 @pytest.mark.parametrize("scale", [1.0, 11.3137])
 def test_forward(T, V, C, scale, dtype):
     ids = _ids("padded" if T > 5 else "uniform", T, V)
@@ -64,7 +64,8 @@ def _backward(ids, d, V, scale, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,V,C", [(1, 1, 1), (2, 1, 3), (5, 700, 16), (63, 9, 128), (64, 9, 128), (65, 9, 128), (129, 2, 8),
                                    (2047, 256, 128), (2049, 1023, 40), (5000, 1024, 9), (3000, 70000, 4), (9000, 31, 520),
-                                   (20011, 256, 128), (700, 1 << 21, 1)])
+                                   (20011, 256, 128), (700, 1 << 21, 1), (2048, 40, 210), (2048, 5, 35),
+                                   (300000, 300, 12), (2500, 60, 210), (4000, 17, 7)])
 @pytest.mark.parametrize("kind", ["uniform", "padded", "one", "skewed"])
 def test_backward(T, V, C, kind, dtype):
     g = torch.Generator().manual_seed(T)
