@@ -77,13 +77,13 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
       for (int u = 0; u < LC; ++u) {
         const int e = (wave * LC + u) * 64 + lane, row = e / L::CPR, ch = L::swap(row, e % L::CPR);
         const int64_t n = p.P - p0, r = min((int64_t)row, (LT ? kleft : n) - 1);
-        loff[u] = (uint32_t)((r * lld + (LT ? min((int64_t)ch * EPC, n - EPC) : ch * EPC)) * sizeof(T));
+        loff[u] = (uint32_t)((r * lld + min((int64_t)ch * EPC, (LT ? n : kleft) - EPC)) * sizeof(T));
       }
 #pragma unroll
       for (int u = 0; u < RC; ++u) {
         const int e = (wave * RC + u) * 64 + lane, row = e / R::CPR, ch = R::swap(row, e % R::CPR);
         const int64_t n = p.Q - q0, r = min((int64_t)row, (RT ? kleft : n) - 1);
-        roff[u] = (uint32_t)((r * rld + (RT ? min((int64_t)ch * EPC, n - EPC) : ch * EPC)) * sizeof(T));
+        roff[u] = (uint32_t)((r * rld + min((int64_t)ch * EPC, (RT ? n : kleft) - EPC)) * sizeof(T));
       }
     };
     offsets(BK);
@@ -95,10 +95,8 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
     auto issue = [&](int s) __attribute__((always_inline)) {
       if (s >= nsteps) return;
       char* dst = smem + s % NBUF * BUF;
-      if constexpr (LT && RT) {
-        const int64_t kleft = p.K - k0 - (int64_t)s * BK;
-        if (kleft < BK) offsets(kleft);
-      }
+      const int64_t kleft = p.K - k0 - (int64_t)s * BK;
+      if (kleft < BK) offsets(kleft);  // (the last step, or none)
 #pragma unroll
       for (int u = 0; u < LC; ++u) lds_copy16_at(reinterpret_cast<const void*>(lat), loff[u], dst + (wave * LC + u) * 1024);
 #pragma unroll
@@ -121,15 +119,16 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
       lds_barrier();
       issue(s + NBUF - 1);  // into the buffer of step s - 1, which every wave has left
       char* buf = smem + s % NBUF * BUF;
-      if constexpr (LT && RT) {
-        const int left = (int)min((int64_t)BK, k1 - k0 - (int64_t)s * BK);
-        if (left < BK) {  // reduction rows past the end count as zero
-          for (int e = threadIdx.x; e < BUF / 16; e += NT) {
-            const int rr = e < L::CHUNKS ? e / L::CPR : (e - L::CHUNKS) % R::CHUNKS / R::CPR;
-            if (rr >= left) reinterpret_cast<f32x4*>(buf)[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-          }
-          __syncthreads();
+      const int left = (int)min((int64_t)BK, k1 - k0 - (int64_t)s * BK);
+      if (left < BK) {  // reduction elements past the end count as zero, on both sides
+        for (int e = threadIdx.x; e < BUF / 16; e += NT) {
+          const bool isl = e < L::CHUNKS;
+          const int ee = isl ? e : (e - L::CHUNKS) % R::CHUNKS;
+          const int row = ee / (isl ? L::CPR : R::CPR), slot = ee % (isl ? L::CPR : R::CPR);
+          const int k = (isl ? LT : RT) ? row : (isl ? L::swap(row, slot) : R::swap(row, slot)) * EPC;
+          if (k >= left) reinterpret_cast<f32x4*>(buf)[e] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
+        __syncthreads();
       }
       compute(buf);
     }
@@ -138,8 +137,38 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
     constexpr int NL = (L::CHUNKS + NT - 1) / NT, NR = (BUF / 16 - L::CHUNKS + NT - 1) / NT;
     const bool lwhole = lld % EPC == 0, rwhole = rld % EPC == 0;
     f32x4 lv[NL], rv[NR];
+    // Steps with rows of the arrays left after them are read without a guard,
+    // vectors at any address from a uniform base: rows past the end repeat the last
+    // one, and a vector that passes a stored row's end takes what follows there
+    // (their products are not stored).
+    uint32_t loff[NL], roff[NR];
+#pragma unroll
+    for (int u = 0; u < NL; ++u) {
+      const int e = min(u * NT + (int)threadIdx.x, L::CHUNKS - 1), row = e / L::CPR, ch = L::swap(row, e % L::CPR);
+      const int64_t n = p.P - p0;
+      loff[u] = (uint32_t)((LT ? row * lld + min((int64_t)ch * EPC, n - 1) : min((int64_t)row, n - 1) * lld + ch * EPC) * sizeof(T));
+    }
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+      const int e = (u * NT + (int)threadIdx.x) % R::CHUNKS, row = e / R::CPR, ch = R::swap(row, e % R::CPR);
+      const int64_t n = p.Q - q0;
+      roff[u] = (uint32_t)((RT ? row * rld + min((int64_t)ch * EPC, n - 1) : min((int64_t)row, n - 1) * rld + ch * EPC) * sizeof(T));
+    }
+    const int64_t lfirst = LT ? k0 * lld + p0 : p0 * lld + k0, rfirst = RT ? k0 * rld + q0 : q0 * rld + k0;
+    const int64_t ladd = LT ? BK * lld : BK, radd = RT ? BK * rld : BK;
     auto load = [&](int s) __attribute__((always_inline)) {
       const int64_t k = k0 + (int64_t)s * BK;
+      if (s < nsteps - 1 && lld >= EPC && rld >= EPC) {
+        const char* lb = reinterpret_cast<const char*>(lsrc + lfirst + s * ladd);
+        const char* rb = reinterpret_cast<const char*>(rsrc + rfirst + s * radd);
+        const char* rl = LO ? reinterpret_cast<const char*>(rlo + rfirst + s * radd) : nullptr;
+#pragma unroll
+        for (int u = 0; u < NL; ++u) __builtin_memcpy(&lv[u], lb + loff[u], 16);
+#pragma unroll
+        for (int u = 0; u < NR; ++u)
+          __builtin_memcpy(&rv[u], (LO && u * NT + (int)threadIdx.x >= R::CHUNKS ? rl : rb) + roff[u], 16);
+        return;
+      }
 #pragma unroll
       for (int u = 0; u < NL; ++u) {
         const int e = u * NT + threadIdx.x, row = e / L::CPR, ch = L::swap(row, e % L::CPR);
@@ -367,10 +396,8 @@ hipError_t launch_prod(const LinGemmParams& p, int tile, bool direct, hipStream_
 }  // namespace
 
 bool lin_direct(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K) {
-  const int64_t epc = 16 / elem_bytes, bk = lin_step(elem_bytes);
-  const bool lok = lin_l_t(prod) ? P % epc == 0 : K % bk == 0;
-  const bool rok = lin_r_t(prod) ? Q % epc == 0 : K % bk == 0;
-  return lok && rok;
+  const int64_t epc = 16 / elem_bytes;
+  return (lin_l_t(prod) ? P : K) % epc == 0 && (lin_r_t(prod) ? Q : K) % epc == 0;
 }
 
 template <typename T>
