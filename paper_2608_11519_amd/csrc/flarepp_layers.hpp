@@ -40,7 +40,7 @@ template <typename T> hipError_t launch_lin_gemm(const LinGemmParams&, int prod,
 
 // The same product for many rows and a strip of outputs (32, 64, 128 or 256
 // wide) whose weights fit the LDS.
-constexpr size_t kLinRowsLds = 144 * 1024;
+constexpr size_t kLinRowsLds = 160 * 1024;
 size_t lin_rows_lds(int elem_bytes, int strip, int64_t K);
 int lin_rows_strip(int prod, int elem_bytes, int64_t Q, int64_t K);
 template <typename T>

@@ -204,6 +204,22 @@ __device__ __forceinline__ void finish4(float (&y)[4], float (&o)[4], const LinG
   }
 }
 
+// A 32 x 32 block (lane (c, g): row c, columns 8 u + 4 g .. + 3 in v[4 u ..]) as the
+// 16-byte vectors 2 m + g of its row, m in order
+template <typename T> __device__ __forceinline__ void row_vectors(const f32x16& v, f32x4* q) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      bf16x8 w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = (__bf16)v[8 * u + e];
+      q[u] = __builtin_bit_cast(f32x4, runs_of_8(w));
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) q[u] = f32x4{v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]};
+  }
+}
 // One 32 x 32 block of C inside the row (Q % EPC == 0): lane (c, g) holds row c,
 // outputs 8 u + 4 g .. + 3 of the block in y[4 u ..].  res, out and pre point to
 // the row's first output of the block (or are null); bias(u) gives the four

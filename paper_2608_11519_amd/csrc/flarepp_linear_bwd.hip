@@ -20,8 +20,8 @@ template <int NT> __device__ __forceinline__ int p_slot(int row, int s) {
 // tokens whose dP = dOut * act'(pre) is formed once, in fp32, and left in LDS as
 // bf16 hi and lo parts; dW += X^T (hi + lo) stays in registers over the chunk, dbias
 // sums dP in fp32, and with DX (K = KT, N = NT, the weights in LDS) dX = hi W^T
-// of the step is stored; else hi goes to memory for dX.  While a step's products
-// run, the next step's dP is formed and the one after is loaded.
+// of the step is stored; else hi goes to memory for dX.  Beside a step's products
+// the next step's dP is formed, and the one after is loaded.
 template <int KT, int NT, bool SLOPE, bool DX> struct Bwd {
   static constexpr int KB = KT / 32, NB = NT / 32, BLOCKS = KB * NB;
   static constexpr int WB = BLOCKS >= 8 ? BLOCKS / 8 : 1;         // blocks of dW per wave, as BK x BN
@@ -32,8 +32,9 @@ template <int KT, int NT, bool SLOPE, bool DX> struct Bwd {
   static_assert(WB <= 4 && LDS <= 160 * 1024 && 512 * 8 * 4 <= 3 * XB + 2 * PARTS * PB, "layout");
 };
 
-template <int KT, int NT, bool SLOPE, bool DX>
+template <int KT, int NT, int ACT, bool DX>
 __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
+  constexpr bool SLOPE = ACT != kActNone;
   using B = Bwd<KT, NT, SLOPE, DX>;
   using X = Tile<T, true, KT>;
   using W = Tile<T, false, KT>;
@@ -84,7 +85,6 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
   for (int e = 0; e < 8; ++e) bias[e] = 0.f;
   auto produce = [&](const Raw& r, int s) __attribute__((always_inline)) {
     char* buf = smem + B::PAT + (s & 1) * (B::PARTS * B::PB);
-    const bool ragged = t0 + (int64_t)(s + 1) * TS > t1;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const int row = r0 + j * RP;
@@ -92,13 +92,10 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
       bf16x8 hi, lo;
       if constexpr (SLOPE) {
         float v[8];
-        with_act(p.act, [&](auto act) __attribute__((always_inline)) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = (float)r.d[j][e] * slope<decltype(act)::value>((float)r.y[j][e]);
-        });
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          if (ragged) v[e] = t < t1 ? v[e] : 0.f;
+          v[e] = (float)r.d[j][e] * slope<ACT>((float)r.y[j][e]);
+          v[e] = t < t1 ? v[e] : 0.f;
           bias[e] += v[e];
           hi[e] = (__bf16)v[e];
           lo[e] = (__bf16)(v[e] - (float)hi[e]);
@@ -106,7 +103,7 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          hi[e] = !ragged || t < t1 ? r.d[j][e] : (__bf16)0.f;
+          hi[e] = t < t1 ? r.d[j][e] : (__bf16)0.f;
           bias[e] += (float)hi[e];
         }
       }
@@ -121,8 +118,8 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
 
   issue_x(0);
   issue_x(1);
-  Raw now, next;
-  load_p(now, 0);
+  Raw first;
+  load_p(first, 0);
   if constexpr (DX) {  // the weights, k-contiguous per input
     const T* w = static_cast<const T*>(p.w);
     constexpr int N16 = KT * NT / 8;
@@ -132,8 +129,7 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
       reinterpret_cast<f32x4*>(smem)[e] = *reinterpret_cast<const f32x4*>(w + (int64_t)row * p.N + b * W::BK + ch * 8);
     }
   }
-  produce(now, 0);
-  load_p(now, 1);  // (a step past the end repeats the last rows and is not used)
+  produce(first, 0);
 
   const int wk = wave / B::WN, wn = wave % B::WN;
   f32x16 acc[B::BK][B::BN];
@@ -144,7 +140,7 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  auto consume = [&](int s, const char* xb, const char* pb, int left) __attribute__((always_inline)) {
+  auto dx_part = [&](int s, const char* pb, int left) __attribute__((always_inline)) {
     if constexpr (DX) {
       // the step's dX: 32 inputs per wave; groups of KB waves take the steps in turn
       constexpr int GROUPS = 8 / B::KB;
@@ -173,7 +169,9 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
         }
       }
     }
-    if (p.part && wave < B::WAVES) {
+  };
+  auto dw_part = [&](const char* xb, const char* pb) __attribute__((always_inline)) {
+    if (wave < B::WAVES) {
 #pragma unroll
       for (int ks = 0; ks < TS / 16; ++ks) {
         bf16x8 xf[B::BK], pf[B::PARTS][B::BN];
@@ -198,12 +196,15 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
     }
   };
 
-  for (int s = 0; s < nsteps; ++s) {
-    // the step's rows of X and its dP are in LDS, and every wave has left the
-    // buffers of the step before
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  // one step: `ahead` holds the next step's raw values, `spare` takes those of
+  // the step after
+  auto turn = [&](int s, Raw& ahead, Raw& spare) __attribute__((always_inline)) {
+    // The step's dP is in LDS, and its X: a wave's own copies are older than
+    // the 2 PARTS NJ loads of the last two turns.  Every wave has left the buffers of
+    // the step before.
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(2 * B::PARTS * NJ) : "memory");
     issue_x(s + 2);
-    load_p(next, s + 2);
+    load_p(spare, s + 2);
     char* xb = smem + B::XAT + s % 3 * B::XB;
     const char* pb = smem + B::PAT + (s & 1) * (B::PARTS * B::PB);
     const int left = (int)min((int64_t)TS, t1 - t0 - (int64_t)s * TS);
@@ -212,16 +213,15 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
         if (e / X::CPR >= left) reinterpret_cast<f32x4*>(xb)[e] = f32x4{0.f, 0.f, 0.f, 0.f};
       lds_barrier();
     }
-    // half of the waves form the next step's dP before this step's products,
-    // half after, so that a SIMD's two waves use its two pipes at once
-    if (wave < 4) {
-      if (s + 1 < nsteps) produce(now, s + 1);
-      consume(s, xb, pb, left);
-    } else {
-      consume(s, xb, pb, left);
-      if (s + 1 < nsteps) produce(now, s + 1);
-    }
-    now = next;
+    dx_part(s, pb, left);
+    dw_part(xb, pb);
+    produce(ahead, s + 1);  // (past the end: zeros into a buffer that is not read)
+  };
+  Raw a, b;
+  load_p(a, 1);  // (a step past the end repeats the last rows)
+  for (int s = 0; s < nsteps; s += 2) {
+    turn(s, a, b);
+    if (s + 1 < nsteps) turn(s + 1, b, a);
   }
 
   if (p.part && wave < B::WAVES) {
@@ -252,21 +252,27 @@ __global__ __launch_bounds__(512) void k_linear_backward(LinBwdParams p) {
   }
 }
 
-template <int KT, int NT, bool SLOPE, bool DX>
+template <int KT, int NT, int ACT, bool DX>
 hipError_t launch_form(const LinBwdParams& p, hipStream_t s) {
-  constexpr int lds = Bwd<KT, NT, SLOPE, DX>::LDS;
-  auto* kernel = k_linear_backward<KT, NT, SLOPE, DX>;
+  constexpr int lds = Bwd<KT, NT, ACT != kActNone, DX>::LDS;
+  auto* kernel = k_linear_backward<KT, NT, ACT, DX>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) return e;
   kernel<<<dim3((unsigned)p.nchunks, (unsigned)(p.N / NT), (unsigned)(p.K / KT)), 512, lds, s>>>(p);
   return hipGetLastError();
 }
+template <int KT, int NT, bool DX> hipError_t launch_act(const LinBwdParams& p, hipStream_t s) {
+  if (p.act == kActGelu) return launch_form<KT, NT, kActGelu, DX>(p, s);
+  if (p.act == kActSilu) return launch_form<KT, NT, kActSilu, DX>(p, s);
+  if (p.act == kActRelu) return launch_form<KT, NT, kActRelu, DX>(p, s);
+  if constexpr (DX) return launch_form<KT, NT, kActNone, DX>(p, s);
+  return hipErrorInvalidValue;
+}
 template <int KT, int NT> hipError_t launch_size(const LinBwdParams& p, bool fused, hipStream_t s) {
-  const bool act = p.act != kActNone;
-  if (fused) {
-    if constexpr (KT * NT <= 128 * 256) return act ? launch_form<KT, NT, true, true>(p, s) : launch_form<KT, NT, false, true>(p, s);
+  if constexpr (KT * NT <= 128 * 256) {
+    if (fused) return launch_act<KT, NT, true>(p, s);
   }
-  if constexpr (KT >= 128 && NT == 128) return launch_form<KT, NT, true, false>(p, s);
+  if constexpr (KT >= 128 && NT == 128) return launch_act<KT, NT, false>(p, s);
   return hipErrorInvalidValue;
 }
 

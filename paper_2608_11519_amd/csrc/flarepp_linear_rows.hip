@@ -13,12 +13,42 @@ namespace {
 // follows the weights' copy.
 // STEPS: K is whole steps of 16 (else rows are read by single elements).
 // WHOLE: Q is whole blocks of 32.
+// Stores NV * 32 bytes (the first `vectors` 16-byte ones) of each of a tile's 32 rows: lane (c, g) holds row c, 16-byte
+// vectors 2 m + g in q[m].  Through 2 KiB of the wave's LDS, 16 rows at a time, so
+// that an instruction stores whole 64- or 128-byte runs of its rows: straight from
+// the product's layout (32 bytes of 32 rows) part of the lines are written twice
+// (131,072 x 128 -> 256 with pre: 161 MB for 134; GELU 56 us, 46 so; 1,048,576 x 128 -> 128
+// with residual 209, 160).
+template <int NV>
+__device__ __forceinline__ void store_rows(char* region, const f32x4 (&q)[NV], void* dst, uint32_t row_bytes, int rows,
+                                           int vectors) {
+  const int lane = lane_id(), g = lane >> 5, c = lane & 31;
+  constexpr int RB = NV * 32, PER = 64 / (2 * NV);  // bytes of a row, rows of an instruction
+  auto slot = [](int row, int v) __attribute__((always_inline)) { return v ^ (row / (256 / RB) & (2 * NV - 1)); };
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if ((c >> 4) == h) {
+#pragma unroll
+      for (int m = 0; m < NV; ++m) *reinterpret_cast<f32x4*>(region + (c & 15) * RB + slot(c & 15, 2 * m + g) * 16) = q[m];
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 16 / PER; ++j) {
+      const int r = j * PER + lane / (2 * NV), v = lane % (2 * NV);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(region + r * RB + slot(r, v) * 16);
+      const int row = 16 * h + r;
+      if (row < rows && v < vectors) *reinterpret_cast<f32x4*>(static_cast<char*>(dst) + (uint32_t)row * row_bytes + v * 16) = x;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // Waves per SIMD: four for the narrowest strip (500,000 x 64 -> 4 25 -> 21 us), two
 // for the others, whose loads ahead are worth more than the waves (1,048,576 x
 // 64 -> 64 101 us, 115 with four; 200,000 x 512 -> 128 82, 109).
-constexpr int rows_waves(int nb) { return nb == 32 ? 4 : 2; }
+constexpr int rows_waves(int nb, int elem_bytes) { return nb == 32 && elem_bytes == 2 ? 4 : 2; }
 template <typename T, bool RT, int NB, bool STEPS, bool WHOLE>
-__global__ __launch_bounds__(512, rows_waves(NB)) void k_linear_rows(LinGemmParams p) {
+__global__ __launch_bounds__(512, rows_waves(NB, sizeof(T))) void k_linear_rows(LinGemmParams p) {
   using F = typename Frag<T>::type;
   using R = Tile<T, RT, NB>;
   constexpr int EPC = R::EPC, BK = R::BK, NQ = NB / 32, KPB = BK / 16;  // steps of a buffer of BK
@@ -110,34 +140,60 @@ __global__ __launch_bounds__(512, rows_waves(NB)) void k_linear_rows(LinGemmPara
       if (seg * SEG + j < KS) step(j);  // uniform
     if (last) {
       const int64_t row = tile * 32 + c;
-      const int64_t at = min(row, p.P - 1) * p.Q + q0;
-      const T* res = p.res ? static_cast<const T*>(p.res) + at : nullptr;
-      T* out = static_cast<T*>(p.out) + at;
-      T* pre = p.pre ? static_cast<T*>(p.pre) + at : nullptr;
+      if constexpr (WHOLE) {
+        const int64_t at = min(row, p.P - 1) * p.Q + q0;
+        const T* res = p.res ? static_cast<const T*>(p.res) + at + 4 * g : nullptr;
+        const int64_t first = scalar64(tile * 32 * p.Q + q0);
+        const int rows = (int)min((int64_t)32, p.P - tile * 32);
+        constexpr int NG = sizeof(T) == 2 && NB >= 64 ? 2 : 1;  // blocks stored together
+        constexpr int NV = NG * (int)sizeof(T);                  // 16-byte vectors of a row per lane
+        char* region = smem + nbuf * R::BYTES + NB * sizeof(float) + wave * 2048;
 #pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        if (q0 + 32 * i < p.Q) {
-          if constexpr (WHOLE) {
-            auto bias = [&](f32x16& y) __attribute__((always_inline)) {
-              if (!p.bias) return;
+        for (int i0 = 0; i0 < NQ; i0 += NG) {
+          if (q0 + 32 * i0 >= p.Q) continue;
+          f32x4 o[NV], y[NV];
+          const int vectors = (int)min((int64_t)2 * NV, (p.Q - q0 - 32 * i0) / EPC);
+#pragma unroll
+          for (int d = 0; d < NG; ++d) {
+            const int i = i0 + d;
+            f32x16 v = acc[i];
+            typename Frag<T>::half r[4];
+            const bool inside = q0 + 32 * i < p.Q;  // uniform
+            if (res && inside) {
+#pragma unroll
+              for (int u = 0; u < 4; ++u) r[u] = load_half(res + 32 * i + 8 * u);
+            }
+            if (p.bias) {
 #pragma unroll
               for (int u = 0; u < 4; ++u) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(lbias + 32 * i + 8 * u + 4 * g);
+                const f32x4 bv = *reinterpret_cast<const f32x4*>(lbias + 32 * i + 8 * u + 4 * g);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) y[4 * u + e] += v[e];
+                for (int e = 0; e < 4; ++e) v[4 * u + e] += bv[e];
               }
-            };
+            }
+            if (p.pre) row_vectors<T>(v, &y[d * sizeof(T)]);
             with_act(p.act, [&](auto act) __attribute__((always_inline)) {
-              epilogue_whole<T, decltype(act)::value>(acc[i], res ? res + 32 * i : nullptr, out + 32 * i,
-                                                      pre ? pre + 32 * i : nullptr, row < p.P, bias);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] = activate<decltype(act)::value>(v[e]);
             });
-          } else {
-            epilogue_parts<T>(acc[i], p, row, q0 + 32 * i);
+            if (res && inside) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] += to_f32(r[e / 4][e % 4]);
+            }
+            row_vectors<T>(v, &o[d * sizeof(T)]);
           }
+          store_rows<NV>(region, o, static_cast<T*>(p.out) + first + 32 * i0, (uint32_t)(p.Q * sizeof(T)), rows, vectors);
+          if (p.pre) store_rows<NV>(region, y, static_cast<T*>(p.pre) + first + 32 * i0, (uint32_t)(p.Q * sizeof(T)), rows, vectors);
         }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+          if (q0 + 32 * i < p.Q) epilogue_parts<T>(acc[i], p, row, q0 + 32 * i);
+      }
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
-      }
     }
     now = next;
     tile = ntile;
@@ -149,7 +205,7 @@ template <typename T, bool RT, int NB, bool STEPS, bool WHOLE>
 hipError_t launch_strip(const LinGemmParams& p, hipStream_t s) {
   const int64_t tiles = (p.P + 31) / 32, strips = (p.Q + NB - 1) / NB;
   const size_t lds = lin_rows_lds(sizeof(T), NB, p.K);
-  const int64_t per_cu = rows_waves(NB) == 4 && 2 * lds <= 160 * 1024 ? 2 : 1;
+  const int64_t per_cu = rows_waves(NB, sizeof(T)) == 4 && 2 * lds <= 160 * 1024 ? 2 : 1;
   const int64_t groups = std::min<int64_t>((tiles + 7) / 8, std::max<int64_t>(1, 256 * per_cu / strips));
   auto* kernel = k_linear_rows<T, RT, NB, STEPS, WHOLE>;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -179,7 +235,7 @@ hipError_t launch_form(const LinGemmParams& p, int strip, hipStream_t s) {
 
 size_t lin_rows_lds(int elem_bytes, int strip, int64_t K) {
   const int64_t bk = lin_step(elem_bytes);
-  return (size_t)((K + bk - 1) / bk) * strip * 128 + strip * sizeof(float);
+  return (size_t)((K + bk - 1) / bk) * strip * 128 + strip * sizeof(float) + 8 * 2048;  // weights, biases, stores
 }
 
 // The strip for a product, or 0 where another kernel has to do: rows of L that

@@ -193,13 +193,17 @@ def test_backward_over_many_tokens(shape, act):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(8192, 16, 32), (8195, 3, 64), (8200, 5, 256), (8193, 64, 4), (8200, 144, 33), (8192, 128, 256),
-                                   (8300, 288, 128), (8192, 512, 256), (8192, 512, 512), (8201, 30, 96)], ids=str)
+                                   (8300, 288, 128), (8192, 512, 256), (8192, 512, 512), (8201, 30, 96), (8195, 64, 160), (8192, 128, 288)], ids=str)
 def test_forward_over_many_rows(shape, dtype):
     """The rows kernel: every strip width, short rows, narrow outputs, two strips."""
     T, K, N = shape
     X, W, b, r, _ = _inputs(T, K, N, dtype, seed=11)
     _check_forward(X, W, b, r, "silu", dtype, *fp.flarepp_linear_forward(X, W, b, act=fp.ACT_SILU, residual=r, keep_pre=True))
     _check_forward(X, W, None, None, "none", dtype, fp.flarepp_linear_forward(X, W), None)
+    buf = torch.full((T * N + 4096,), 7.0, dtype=X.dtype, device="cuda")  # what follows the last row stays
+    out = buf[:T * N].view(T, N)
+    fp.flarepp_linear_forward(X, W, b, act=fp.ACT_SILU, residual=r, out=out)
+    assert torch.equal(out, fp.flarepp_linear_forward(X, W, b, act=fp.ACT_SILU, residual=r)) and (buf[T * N:] == 7).all()
 
 
 @pytest.mark.parametrize("shape", [(16500, 1024, 1032), (12544, 128, 1024)], ids=str)
