@@ -49,7 +49,7 @@ def parse_args(argv=None):
     ap.add_argument("--no-backward", action="store_true", help="skip the mixer-backward timing")
     ap.add_argument("--no-block", action="store_true", help="skip the pre-norm residual block timing")
     ap.add_argument("--no-train-pair", action="store_true",
-                    help="skip the training forward + backward-from-saved timing")
+                    help="skip the training forward + backward-from-saved timing, and the training step's")
     ap.add_argument("--cpu-seconds", type=float, default=10.0,
                     help="minimum host seconds spent timing the oracle")
     ap.add_argument("--stage-reps", type=int, default=20,
@@ -347,6 +347,61 @@ def time_backward(args, w, t, use_graph):
             "train_pair_ms": None if ms_train is None else round(ms_train, 5)}
 
 
+def time_train_step(args, w, t, use_graph):
+    """A complete training step of the mixer on the same workload: the
+    training pair for a seeded dO, then AdamW on the six parameters (fp32
+    masters; with bf16 the step also writes the weights the next forward
+    reads).  Where X is an embedding (x_kind), the lookup, the table's gradient
+    and its update are part of the step."""
+    import torch
+
+    from paper_2608_11519_amd import flarepp as fp
+    from paper_2608_11519_amd import inputs as inp
+
+    dcode = fp.BF16 if w.dtype == "bf16" else fp.F32
+    dev, dt = t["X"].device, t["X"].dtype
+    dO = torch.from_numpy(inp.make_tensor((w.B, w.N, w.C), 100, w.dtype)).to(dev, dt)
+    ws = torch.empty(fp.flarepp_mixer_backward_workspace_bytes(dcode, w.B, w.N, w.C, w.H, w.M),
+                     dtype=torch.uint8, device=dev)
+    f32 = dict(dtype=torch.float32, device=dev)
+    names = ("Wk", "Wv", "Wkt", "Wvt", "Wo", "seeds")
+    weights = {k: t[k].clone() for k in names}
+    grads = {"d" + k: torch.empty(t[k].shape, **f32) for k in names}
+    grads["dX"] = torch.empty((w.B, w.N, w.C), **f32)
+    X, O = t["X"], torch.empty_like(t["X"])
+    table = ids = None
+    if w.x_kind == "embedding":
+        table = torch.from_numpy(inp.make_tensor((inp.EMBED_VOCAB, w.C), 101, w.dtype)).to(dev, dt)
+        ids = torch.randint(0, inp.EMBED_VOCAB, (w.B, w.N), device=dev)
+        X, grads["dtable"] = torch.empty_like(t["X"]), torch.empty((inp.EMBED_VOCAB, w.C), **f32)
+        weights["table"] = table
+
+    def param(k, v):
+        p = v.float() if w.dtype == "bf16" else v
+        return dict(p=p, g=grads["d" + k], m=torch.zeros(v.shape, **f32), v=torch.zeros(v.shape, **f32), weight_decay=0.01,
+                    p_low=v if w.dtype == "bf16" else None)
+
+    plan = fp.flarepp_adamw_plan([param(k, v) for k, v in weights.items()])
+    six = [weights[k] for k in names]
+
+    def optimizer():
+        fp.flarepp_adamw_step(plan, lr=1e-5, step=1)
+
+    def step():
+        if ids is not None:
+            fp.flarepp_embedding_forward(ids, table, out=X)
+        fp.flarepp_mixer_forward_train(X, *six, H=w.H, ws=ws, out=O)
+        fp.flarepp_mixer_backward_from_saved(X, *six, dO, H=w.H, ws=ws, out={k: grads[k] for k in grads if k != "dtable"})
+        if ids is not None:
+            fp.flarepp_embedding_backward(ids, grads["dX"], V=inp.EMBED_VOCAB, out=grads["dtable"])
+        optimizer()
+
+    ms = _time_steps(args, step, use_graph)
+    return {"ms_per_step": round(ms, 5), "tokens_per_s": round(w.B * w.N / (ms * 1e-3), 1),
+            "optimizer_ms": round(_time_steps(args, optimizer, use_graph), 5),
+            "parameters": sum(v.numel() for v in weights.values()), "embedding": ids is not None}
+
+
 def time_flare(args, w, t, use_graph):
     """The fixed-query FLARE mixer (Sec. 3.1) on the same workload and
     weights (its learned queries: the seeds), timed like the FLARE++ step:
@@ -499,6 +554,7 @@ def main(argv=None):
     torch.cuda.synchronize()
     flare = time_flare(args, w, t, graph is not None)
     backward = None if args.no_backward else time_backward(args, w, t, graph is not None)
+    train = None if args.no_backward or args.no_train_pair else time_train_step(args, w, t, graph is not None)
     block = None if args.no_block else time_block(args, w, t, graph is not None, ms_per_step)
     work = stage_work(w, fused)
     stages = {n: {"ms": round(stage_ms[n], 5), **roofline(work[n], stage_ms[n], w.dtype)}
@@ -546,6 +602,8 @@ def main(argv=None):
         out["block"] = block
     if backward is not None:
         out["backward"] = backward
+    if train is not None:
+        out["train_step"] = train
     if not args.no_cpu_baseline:
         print("[bench] timing the oracle on the host", file=sys.stderr, flush=True)
         out["cpu_baseline"] = cpu_baseline(w, d, args.cpu_seconds)
