@@ -68,14 +68,15 @@ template <typename V> __device__ __forceinline__ V load4(const void* p, int64_t 
 // One block of 256 elements per wave and turn, four elements per lane.
 template <bool Q8>
 __global__ __launch_bounds__(256) void k_adamw(AdamwParams p) {
-  int k = 0;
-  for (int step = 32; step > 0; step /= 2)
-    if (k + step < p.count && (int)blockIdx.x >= p.t[k + step].first) k += step;
+  // this workgroup's tensor: one compare per lane (a search would wait for the
+  // argument's memory at every step)
+  const int mine = lane_id() < p.count && p.first[lane_id() < kAdamwPerLaunch ? lane_id() : 0] <= (int)blockIdx.x;
+  const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(mine)) - 1;
   const AdamwTensor& t = p.t[k];
   const AdamwSchedule now = p.schedule ? *p.schedule : p.now;
   const float keep = (float)(1.0 - now.lr * t.decay);
   const int lane = lane_id();
-  const int64_t base = ((int64_t)((int)blockIdx.x - t.first) * 4 + wave_id()) * (kAdamwBlock * kAdamwTurns);
+  const int64_t base = ((int64_t)((int)blockIdx.x - p.first[k]) * 4 + wave_id()) * (kAdamwBlock * kAdamwTurns);
   f32x4 pv[kAdamwTurns], gv[kAdamwTurns], mv[kAdamwTurns], vv[kAdamwTurns];
   uint32_t mc[kAdamwTurns], vc[kAdamwTurns];
   float ms[kAdamwTurns], vs[kAdamwTurns];

@@ -122,9 +122,9 @@ struct AdamwTensor {
   float* p; const float* g; void* m; void* v; float* m_scale; float* v_scale; void* p_low;
   int64_t n;
   double decay;
-  int first;   // blocks of the tensors before it in this launch
 };
 struct AdamwParams {
+  int first[kAdamwPerLaunch];  // workgroups of the tensors before each one
   AdamwTensor t[kAdamwPerLaunch];
   int count, blocks;
   float b1, a1, b2, a2, eps;

@@ -365,8 +365,9 @@ int adamw_entry(int state, int64_t count, const flarepp_adamw_tensor* tensors, d
       const flarepp_adamw_tensor& t = tensors[i];
       const int64_t more = cdiv(t.n, kAdamwUnit);
       if (p.count && blocks + more > (1 << 30)) break;
+      p.first[p.count] = (int)blocks;
       p.t[p.count++] = {(float*)t.p, (const float*)t.g, t.m, t.v, (float*)t.m_scale, (float*)t.v_scale, t.p_low,
-                        t.n, t.weight_decay, (int)blocks};
+                        t.n, t.weight_decay};
       blocks += more;
     }
     p.blocks = (int)blocks;
