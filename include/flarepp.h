@@ -414,8 +414,8 @@ FLAREPP_API int flarepp_mixer_stage(int stage, int dtype, int64_t B, int64_t N, 
  * end.  Activations: RELU max(P, 0); GELU P Phi(P) with the normal
  * distribution's Phi; SILU P / (1 + exp(-P)).
  * T <= 2^30, K and N <= 65536 of any parity, T * max(K, N) <= 2^40 (UNSUPPORTED
- * beyond).  `out` may be `residual` itself; no other output may overlap an
- * input or another output.  Workspace: flarepp_linear_workspace_bytes(...)
+ * beyond).  `out` may be `residual` itself; otherwise an output (or the
+ * workspace) that overlaps another buffer of the call is INVALID_ARG.  Workspace: flarepp_linear_workspace_bytes(...)
  * bytes (0 for an invalid shape; 256, the least, where the call uses none: ws
  * may then be NULL).
  * ------------------------------------------------------------------------- */
@@ -439,8 +439,7 @@ FLAREPP_API int flarepp_linear_forward(int dtype, int act, int64_t T, int64_t K,
  * With bf16, dX is made of dP rounded to bf16, dW of dP as two bf16 parts (hi
  * + lo, ~16 bits: the sums over the tokens keep more bits than one part has),
  * dbias of dP in fp32.  Sums over the tokens have a fixed order.
- * Sizes and errors as for the forward; no output may overlap an input or
- * another output.  Workspace: flarepp_linear_backward_workspace_bytes(...)
+ * Sizes, overlaps and errors as for the forward.  Workspace: flarepp_linear_backward_workspace_bytes(...)
  * bytes (0 for an invalid shape).
  * ------------------------------------------------------------------------- */
 FLAREPP_API size_t flarepp_linear_backward_workspace_bytes(int dtype, int act, int64_t T, int64_t K, int64_t N);
@@ -461,8 +460,8 @@ FLAREPP_API int flarepp_linear_backward(int dtype, int act, int64_t T, int64_t K
  * symbol, and the sums, fp32, run over ascending positions in an order that
  * depends on the ids alone.  Workspace:
  * flarepp_embedding_backward_workspace_bytes(...) bytes (0 for an invalid
- * shape; 256, the least, where the call uses none: ws may then be NULL).  No
- * output may overlap an input.
+ * shape; 256, the least, where the call uses none: ws may then be NULL).
+ * Overlapping buffers are INVALID_ARG.
  * ------------------------------------------------------------------------- */
 FLAREPP_API int flarepp_embedding_forward(int dtype, int64_t T, int64_t V, int64_t C, const int64_t* ids,
                                           const void* table, float scale, void* out, void* stream);

@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -62,6 +63,23 @@ int check_ws(const void* ws, size_t have, size_t need) {
   if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(FLAREPP_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
   if (have < need)
     return fail(FLAREPP_ERR_WORKSPACE, "workspace of %zu bytes is smaller than the %zu required", have, need);
+  return FLAREPP_OK;
+}
+
+// A buffer that a call reads or writes; no written one may overlap another.
+struct Range {
+  uintptr_t from, to;
+  bool written;
+};
+Range range(const void* p, int64_t bytes, bool written) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  return {a, p ? a + (uintptr_t)bytes : a, written};
+}
+int check_disjoint(std::initializer_list<Range> rs) {
+  for (const Range* x = rs.begin(); x != rs.end(); ++x)
+    for (const Range* y = x + 1; y != rs.end(); ++y)
+      if ((x->written || y->written) && x->from < y->to && y->from < x->to)
+        return fail(FLAREPP_ERR_INVALID_ARG, "an output overlaps another buffer of the call");
   return FLAREPP_OK;
 }
 
@@ -283,12 +301,7 @@ size_t embed_ws(EmbedGradParams& p, void* base) {
 }
 
 // ---- optimiser -----------------------------------------------------------------------
-struct Range {
-  uintptr_t from, to;
-  bool written;
-};
-
-// A buffer that a step writes may overlap no other buffer of the step.
+// The same for many buffers.
 int check_ranges(std::vector<Range>& r) {
   std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
   uintptr_t any = 0, written = 0;
@@ -347,8 +360,7 @@ int adamw_entry(int state, int64_t count, const flarepp_adamw_tensor* tensors, d
         continue;
       }
       TRY(check_ptr(b.p, b.name));
-      const uintptr_t a = reinterpret_cast<uintptr_t>(b.p);
-      ranges.push_back({a, a + (uintptr_t)b.bytes, b.written});
+      ranges.push_back(range(b.p, b.bytes, b.written));
     }
   }
   TRY(check_ranges(ranges));
@@ -394,9 +406,12 @@ int flarepp_linear_forward(int dtype, int act, int64_t T, int64_t K, int64_t N, 
   TRY(check_ptr(residual, "residual", true));
   TRY(check_ptr(out, "out"));
   TRY(check_ptr(pre, "pre", true));
-  if (out == X || out == W || pre == X || pre == W || pre == out || (pre && pre == residual))
-    return fail(FLAREPP_ERR_INVALID_ARG, "out and pre must not be X, W or each other, nor pre the residual");
-  TRY(check_ws(ws, ws_bytes, lin_plan(kLinForward, dtype == FLAREPP_F32 ? 4 : 2, T, N, K).part_bytes));
+  const int64_t bs = dtype == FLAREPP_F32 ? 4 : 2;
+  const size_t need = lin_plan(kLinForward, (int)bs, T, N, K).part_bytes;
+  TRY(check_ws(ws, ws_bytes, need));
+  TRY(check_disjoint({range(X, bs * T * K, false), range(W, bs * K * N, false), range(bias, bs * N, false),
+                      range(residual == out ? nullptr : residual, bs * T * N, false), range(out, bs * T * N, true),
+                      range(pre, bs * T * N, true), range(need ? ws : nullptr, need, true)}));
   hipStream_t s = static_cast<hipStream_t>(stream);
   return dtype == FLAREPP_F32 ? run_linear<float>(act, T, K, N, X, W, bias, residual, out, pre, ws, s)
                               : run_linear<__bf16>(act, T, K, N, X, W, bias, residual, out, pre, ws, s);
@@ -418,9 +433,13 @@ int flarepp_linear_backward(int dtype, int act, int64_t T, int64_t K, int64_t N,
   TRY(check_ptr(dX, "dX", true));
   TRY(check_ptr(dW, "dW", true));
   TRY(check_ptr(dbias, "dbias", true));
-  if (dX && (dX == X || dX == W || dX == pre || dX == dOut))
-    return fail(FLAREPP_ERR_INVALID_ARG, "dX must not be one of the inputs");
-  TRY(check_ws(ws, ws_bytes, flarepp_linear_backward_workspace_bytes(dtype, act, T, K, N)));
+  const int64_t bs = dtype == FLAREPP_F32 ? 4 : 2;
+  const size_t need = flarepp_linear_backward_workspace_bytes(dtype, act, T, K, N);
+  TRY(check_ws(ws, ws_bytes, need));
+  TRY(check_disjoint({range(dW ? X : nullptr, bs * T * K, false), range(dX ? W : nullptr, bs * K * N, false),
+                      range(act != FLAREPP_ACT_NONE ? pre : nullptr, bs * T * N, false), range(dOut, bs * T * N, false),
+                      range(dX, bs * T * K, true), range(dW, 4 * K * N, true), range(dbias, 4 * N, true),
+                      range(ws, need, true)}));
   hipStream_t s = static_cast<hipStream_t>(stream);
   return dtype == FLAREPP_F32 ? run_linear_backward<float>(dtype, act, T, K, N, X, W, pre, dOut, dX, dW, dbias, ws, s)
                               : run_linear_backward<__bf16>(dtype, act, T, K, N, X, W, pre, dOut, dX, dW, dbias, ws, s);
@@ -432,7 +451,8 @@ int flarepp_embedding_forward(int dtype, int64_t T, int64_t V, int64_t C, const 
   TRY(check_ptr(ids, "ids"));
   TRY(check_ptr(table, "table"));
   TRY(check_ptr(out, "out"));
-  if (out == table || out == ids) return fail(FLAREPP_ERR_INVALID_ARG, "out must not be one of the inputs");
+  const int64_t bs = dtype == FLAREPP_F32 ? 4 : 2;
+  TRY(check_disjoint({range(ids, 8 * T, false), range(table, bs * V * C, false), range(out, bs * T * C, true)}));
   EmbedParams p{ids, table, out, T, V, C, scale};
   hipStream_t s = static_cast<hipStream_t>(stream);
   HIPTRY(dtype == FLAREPP_F32 ? launch_embed<float>(p, s) : launch_embed<__bf16>(p, s));
@@ -452,10 +472,12 @@ int flarepp_embedding_backward(int dtype, int64_t T, int64_t V, int64_t C, const
   TRY(check_ptr(ids, "ids"));
   TRY(check_ptr(dOut, "dOut"));
   TRY(check_ptr(dTable, "dTable"));
-  if ((const void*)dTable == dOut) return fail(FLAREPP_ERR_INVALID_ARG, "dTable must not be dOut");
   EmbedGradParams p{};
   p.ids = ids; p.dout = dOut; p.T = T; p.V = V; p.C = C; p.scale = scale; p.dtable = dTable;
-  TRY(check_ws(ws, ws_bytes, embed_ws(p, ws)));
+  const size_t need = embed_ws(p, ws);
+  TRY(check_ws(ws, ws_bytes, need));
+  TRY(check_disjoint({range(ids, 8 * T, false), range(dOut, (dtype == FLAREPP_F32 ? 4 : 2) * T * C, false),
+                      range(dTable, 4 * V * C, true), range(need ? ws : nullptr, need, true)}));
   hipStream_t s = static_cast<hipStream_t>(stream);
   HIPTRY(dtype == FLAREPP_F32 ? launch_embed_grad<float>(p, s) : launch_embed_grad<__bf16>(p, s));
   return api_ok();

@@ -266,7 +266,7 @@ def test_leading_dimensions_and_in_place_residual(dtype):
     assert torch.equal(fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, residual=r, out=r), ref)
 
 
-@pytest.mark.parametrize("shape", [(4000, 64, 128), (33, 1030, 12)], ids=str)
+@pytest.mark.parametrize("shape", [(4000, 64, 128), (33, 1030, 12), (9000, 128, 256), (8200, 256, 256), (16500, 1024, 1024)], ids=str)
 def test_graph_replays_and_streams(shape):
     X, W, b, r, d = _inputs(*shape, "bf16", seed=9)
     out, pre = fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, keep_pre=True)

@@ -11,7 +11,7 @@ import torch
 from oracle import layers_oracle as orc
 from paper_2608_11519_amd import flarepp as fp
 
-_P = [ctypes.c_void_p(4096 * (i + 1)) for i in range(16)]  # aligned, never dereferenced: validation fails first
+_P = [ctypes.c_void_p(i + 1 << 44) for i in range(16)]  # aligned, far apart, never dereferenced: validation fails first
 BAD = ctypes.c_void_p(4096 + 8)
 
 
@@ -48,10 +48,15 @@ def test_linear_refuses_pointers():
         if i in (0, 1, 4):
             ptrs[i] = None
             assert _forward(ptrs=ptrs) == fp.ERR_INVALID_ARG
-    for i, j in ((4, 0), (4, 1), (5, 0), (5, 1), (5, 4), (5, 3)):
-        ptrs = list(_P[:6])
-        ptrs[i] = ptrs[j]
-        assert _forward(ptrs=ptrs) == fp.ERR_INVALID_ARG
+    for i, j in ((4, 0), (4, 1), (4, 2), (5, 0), (5, 1), (5, 4), (5, 3)):
+        for at in (0, 16, -16):  # the same buffer, or one that reaches into it
+            ptrs = list(_P[:6])
+            ptrs[i] = ctypes.c_void_p(ptrs[j].value + at)
+            assert _forward(ptrs=ptrs) == fp.ERR_INVALID_ARG and "overlap" in fp.last_error()
+    ptrs = list(_P[:6])
+    ptrs[3] = ctypes.c_void_p(ptrs[4].value + 16)  # in place, but not quite
+    assert _forward(ptrs=ptrs) == fp.ERR_INVALID_ARG
+    assert _forward(ws=_P[4]) == fp.ERR_INVALID_ARG
     for i in range(7):  # X, W, pre, dOut, dX, dW, dbias
         ptrs = list(_P[:7])
         ptrs[i] = BAD
@@ -60,10 +65,11 @@ def test_linear_refuses_pointers():
             ptrs[i] = None
             assert _backward(ptrs=ptrs) == fp.ERR_INVALID_ARG
     assert _backward(ptrs=_P[:4] + [None] * 3) == fp.ERR_INVALID_ARG
-    for j in range(4):
-        ptrs = list(_P[:7])
-        ptrs[4] = ptrs[j]
-        assert _backward(ptrs=ptrs) == fp.ERR_INVALID_ARG
+    for i in (4, 5, 6):
+        for j in range(7):
+            ptrs = list(_P[:7])
+            ptrs[i] = ptrs[j]
+            assert i == j or _backward(ptrs=ptrs) == fp.ERR_INVALID_ARG
 
 
 def test_linear_workspaces():
