@@ -37,6 +37,7 @@ def command(out: str = LIB):
         # VALU, and the AGPR form would copy them around every MFMA
         "-mllvm", "-amdgpu-mfma-vgpr-form=1",
         "-fvisibility=hidden", "-Wall", "-Wno-unused-result",
+        "-parallel-jobs=8",  # of the sources below
         "-o", out,
     ] + [os.path.join(CSRC, s) for s in SOURCES]
 

@@ -38,6 +38,9 @@ constexpr int lin_step(int elem_bytes) { return 128 / elem_bytes; }
 bool lin_direct(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K);
 template <typename T> hipError_t launch_lin_gemm(const LinGemmParams&, int prod, int tile, bool direct, hipStream_t);
 
+// The input and the weight gradient in one launch, both in 64 x 64 tiles
+template <typename T> hipError_t launch_lin_pair(const LinGemmParams& dx, const LinGemmParams& dw, bool direct, hipStream_t);
+
 // The same product for many rows and a strip of outputs (32, 64, 128 or 256
 // wide) whose weights fit the LDS.
 constexpr size_t kLinRowsLds = 160 * 1024;

@@ -130,7 +130,7 @@ LinPlan lin_plan(int prod, int bs, int64_t P, int64_t Q, int64_t K) {
   int64_t bp, bq;
   if (Q <= 32 && P > 64) { pl.tile = kTile128x32; bp = 128; bq = 32; }
   else if (P <= 32 && Q > 64) { pl.tile = kTile32x128; bp = 32; bq = 128; }
-  else if (P > 64 && Q > 64 && (weight || cdiv(P, 128) * cdiv(Q, 128) >= 256)) { pl.tile = kTile128; bp = bq = 128; }
+  else if (P > 64 && Q > 64 && (weight ? K >= kLinRowsFrom : cdiv(P, 128) * cdiv(Q, 128) >= 256)) { pl.tile = kTile128; bp = bq = 128; }
   else { pl.tile = kTile64; bp = bq = 64; }
   if (pl.tile == kTile128 && !weight && bs == 2 && lin_direct(prod, bs, P, Q, K)) {
     // 256 x 256 where they fill the CUs' rounds to three quarters and pass the
@@ -196,7 +196,7 @@ LinBwdWs lin_bwd_ws(void* base, int dtype, int act, int64_t rows, int64_t K, int
     if (dtype == FLAREPP_BF16) w.dp_lo = cv.take(bs * rows * N);
   }
   // (few rows: one chunk, and no sum of partials)
-  w.chunk = rows <= 128 ? rows : std::max<int64_t>(64, cdiv(rows, 512));
+  w.chunk = rows <= 128 ? rows : std::max<int64_t>(32, cdiv(rows, 512));
   w.pass = dtype == FLAREPP_BF16 && rows >= kLinBwdFrom && lin_bwd_tile(K, N, act, w.kt, w.nt, w.fused);
   if (w.pass) {  // a workgroup per CU, of two steps at least
     const int64_t tiles = (K / w.kt) * (N / w.nt);
@@ -252,20 +252,25 @@ int run_linear_backward(int dtype, int act, int64_t rows, int64_t K, int64_t N, 
     p.part_ld = w.bias_ld; p.nchunks = w.nchunks; p.chunk = w.chunk;
     HIPTRY(launch_lin_slope<T>(p, s));
   }
-  if (dX) {
-    LinGemmParams p = lin_params(w.dx, rows, K, N, dp, W, w.part);
-    p.out = dX;
-    if (w.dx.strip) HIPTRY(launch_lin_rows<T>(p, kLinInput, w.dx.strip, s));
-    else HIPTRY(launch_lin_gemm<T>(p, kLinInput, w.dx.tile, w.dx.direct, s));
-    if (p.part) HIPTRY(launch_lin_finish<T>(p, s));
-  }
+  LinGemmParams px = lin_params(w.dx, rows, K, N, dp, W, w.part);
+  px.out = dX;
+  LinGemmParams pw = lin_params(w.dw, K, N, rows, X, dp, w.part);
+  pw.r_lo = act != FLAREPP_ACT_NONE ? w.dp_lo : nullptr;
   LinSumParams sums{};
   if (dW) {
-    LinGemmParams p = lin_params(w.dw, K, N, rows, X, dp, w.part);
-    p.r_lo = act != FLAREPP_ACT_NONE ? w.dp_lo : nullptr;
-    if (p.part) sums.job[sums.njobs++] = {p.part, p.part_stride, K * N, p.splits, dW};
-    else p.part = dW;
-    HIPTRY(launch_lin_gemm<T>(p, kLinWeight, w.dw.tile, w.dw.direct, s));
+    if (pw.part) sums.job[sums.njobs++] = {pw.part, pw.part_stride, K * N, pw.splits, dW};
+    else pw.part = dW;
+  }
+  // small products go together (the partial sums of both never share the workspace)
+  if (dX && dW && !px.part && !w.dx.strip && w.dx.tile == kTile64 && w.dw.tile == kTile64) {
+    HIPTRY(launch_lin_pair<T>(px, pw, w.dx.direct && w.dw.direct, s));
+  } else {
+    if (dX) {
+      if (w.dx.strip) HIPTRY(launch_lin_rows<T>(px, kLinInput, w.dx.strip, s));
+      else HIPTRY(launch_lin_gemm<T>(px, kLinInput, w.dx.tile, w.dx.direct, s));
+      if (px.part) HIPTRY(launch_lin_finish<T>(px, s));
+    }
+    if (dW) HIPTRY(launch_lin_gemm<T>(pw, kLinWeight, w.dw.tile, w.dw.direct, s));
   }
   if (dbias && w.nchunks > 1) sums.job[sums.njobs++] = {w.bias_part, w.bias_ld, N, w.nchunks, dbias};
   if (sums.njobs) HIPTRY(launch_lin_sum(sums, s));

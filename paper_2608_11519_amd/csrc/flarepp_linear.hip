@@ -7,22 +7,24 @@ namespace flarepp {
 namespace {
 
 // ---- the product -------------------------------------------------------------------
+template <typename T, int PROD, bool LO, int BP, int BQ, int NBUF, int KB> constexpr int lin_lds() {
+  return (Tile<T, lin_l_t(PROD), BP, KB>::BYTES + Tile<T, lin_r_t(PROD), BQ, KB>::BYTES * (LO ? 2 : 1)) * NBUF;
+}
 template <typename T, int PROD, bool LO, int BP, int BQ, int WP, int WQ, bool DIRECT, int NBUF, int KB>
-__global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
+__device__ __forceinline__ void linear_tile(const LinGemmParams& p, int block, char* smem) {
   constexpr bool LT = lin_l_t(PROD), RT = lin_r_t(PROD);
   using L = Tile<T, LT, BP, KB>;
   using R = Tile<T, RT, BQ, KB>;
   constexpr int EPC = L::EPC, BK = L::BK, NP = BP / WP / 32, NQ = BQ / WQ / 32, NW = WP * WQ, NT = 64 * NW;
   constexpr int BUF = L::BYTES + R::BYTES * (LO ? 2 : 1);
-  __shared__ __attribute__((aligned(16))) char smem[BUF * NBUF];
   const int lane = lane_id(), wave = wave_id(), g = lane >> 5, c = lane & 31;
   const int wp = wave / WQ, wq = wave % WQ;
 
   // tiles in the order q, p, split; the workgroups of one XCD (dealt out in
   // turn) take a run of them, so they share the rows of L and R in its L2
   const int64_t ntp = (p.P + BP - 1) / BP, ntq = (p.Q + BQ - 1) / BQ, total = ntp * ntq * p.splits;
-  const int64_t per = (total + 7) / 8, tile = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int64_t)(blockIdx.x >> 3) >= per || tile >= total) return;  // whole workgroup, before any barrier
+  const int64_t per = (total + 7) / 8, tile = (block & 7) * per + (block >> 3);
+  if ((block >> 3) >= per || tile >= total) return;  // whole workgroup, before any barrier
   const int64_t q0 = tile % ntq * BQ, p0 = tile / ntq % ntp * BP;
   const int z = (int)(tile / (ntq * ntp));
   const int64_t k0 = z * p.kchunk, k1 = min(p.K, k0 + p.kchunk);
@@ -248,6 +250,23 @@ __global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
   });
 }
 
+template <typename T, int PROD, bool LO, int BP, int BQ, int WP, int WQ, bool DIRECT, int NBUF, int KB>
+__global__ __launch_bounds__(64 * WP * WQ) void k_linear(LinGemmParams p) {
+  __shared__ __attribute__((aligned(16))) char smem[lin_lds<T, PROD, LO, BP, BQ, NBUF, KB>()];
+  linear_tile<T, PROD, LO, BP, BQ, WP, WQ, DIRECT, NBUF, KB>(p, blockIdx.x, smem);
+}
+
+// Both products of a small backward in one launch (64 x 64 tiles): the input
+// gradient's workgroups, then the weight gradient's.
+template <typename T, bool LO, bool DIRECT>
+__global__ __launch_bounds__(256) void k_linear_pair(LinGemmParams dx, LinGemmParams dw, int first) {
+  constexpr int NBUF = DIRECT ? 3 : 2;
+  constexpr int A = lin_lds<T, kLinInput, false, 64, 64, NBUF, 128>(), B = lin_lds<T, kLinWeight, LO, 64, 64, NBUF, 128>();
+  __shared__ __attribute__((aligned(16))) char smem[A > B ? A : B];
+  if ((int)blockIdx.x < first) linear_tile<T, kLinInput, false, 64, 64, 2, 2, DIRECT, NBUF, 128>(dx, blockIdx.x, smem);
+  else linear_tile<T, kLinWeight, LO, 64, 64, 2, 2, DIRECT, NBUF, 128>(dw, blockIdx.x - first, smem);
+}
+
 // ---- epilogue of a product whose reduction was split ----------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void k_linear_finish(LinGemmParams p) {
@@ -393,6 +412,10 @@ hipError_t launch_prod(const LinGemmParams& p, int tile, bool direct, hipStream_
   }
 }
 
+int64_t tile64_blocks(const LinGemmParams& p) {
+  return ((p.P + 63) / 64 * ((p.Q + 63) / 64) * p.splits + 7) / 8 * 8;
+}
+
 }  // namespace
 
 bool lin_direct(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K) {
@@ -411,6 +434,21 @@ hipError_t launch_lin_gemm(const LinGemmParams& p, int prod, int tile, bool dire
 }
 template hipError_t launch_lin_gemm<float>(const LinGemmParams&, int, int, bool, hipStream_t);
 template hipError_t launch_lin_gemm<__bf16>(const LinGemmParams&, int, int, bool, hipStream_t);
+
+template <typename T>
+hipError_t launch_lin_pair(const LinGemmParams& dx, const LinGemmParams& dw, bool direct, hipStream_t s) {
+  const int64_t first = tile64_blocks(dx), grid = first + tile64_blocks(dw);
+  auto go = [&](auto lo, auto dir) {
+    k_linear_pair<T, decltype(lo)::value != 0, decltype(dir)::value != 0><<<dim3((unsigned)grid), 256, 0, s>>>(dx, dw, (int)first);
+    return hipGetLastError();
+  };
+  if constexpr (sizeof(T) == 2) {
+    if (dw.r_lo) return direct ? go(ActC<1>{}, ActC<1>{}) : go(ActC<1>{}, ActC<0>{});
+  }
+  return direct ? go(ActC<0>{}, ActC<1>{}) : go(ActC<0>{}, ActC<0>{});
+}
+template hipError_t launch_lin_pair<float>(const LinGemmParams&, const LinGemmParams&, bool, hipStream_t);
+template hipError_t launch_lin_pair<__bf16>(const LinGemmParams&, const LinGemmParams&, bool, hipStream_t);
 
 template <typename T>
 hipError_t launch_lin_finish(const LinGemmParams& p, hipStream_t s) {

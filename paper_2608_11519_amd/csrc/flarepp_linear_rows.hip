@@ -250,7 +250,7 @@ int lin_rows_strip(int prod, int elem_bytes, int64_t Q, int64_t K) {
   int strip = 32;
   while (strip < widest && strip < Q) strip *= 2;
   while (strip > 32 && lin_rows_lds(elem_bytes, strip, K) > kLinRowsLds) strip /= 2;
-  return lin_rows_lds(elem_bytes, strip, K) <= kLinRowsLds && (Q + strip - 1) / strip <= (K <= 512 ? 2 : 1) ? strip : 0;
+  return lin_rows_lds(elem_bytes, strip, K) <= kLinRowsLds && (Q + strip - 1) / strip <= (K < 512 ? 2 : 1) ? strip : 0;
 }
 
 template <typename T>
