@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256) void k_embed_scatter(EmbedGradParams p, int pa
   }
 }
 
-// Sums over the runs of equal symbols inside chunks of kEmbedChunk sorted
+// Sums over the runs of equal symbols inside chunks of p.chunk sorted
 // positions, 2^cl lanes per chunk and strip of columns.  A run inside one
 // chunk is a row of the result; parts of longer runs go to part[chunk][0]
 // (began before the chunk) or [1] (goes on after it).
@@ -212,7 +212,7 @@ template <typename T, int VEC, bool WHOLE>
 __global__ __launch_bounds__(256) void k_embed_runs(EmbedGradParams p, int cl) {
   const int64_t col = (((int64_t)blockIdx.y << cl) + (threadIdx.x & ((1 << cl) - 1))) * VEC;
   const int64_t chunk = ((int64_t)blockIdx.x << (8 - cl)) + (threadIdx.x >> cl);
-  const int64_t i0 = chunk * kEmbedChunk, i1 = min(p.T, i0 + kEmbedChunk);
+  const int64_t i0 = chunk * p.chunk, i1 = min(p.T, i0 + p.chunk);
   if (i0 >= p.T || col >= p.C) return;
   const uint32_t* key = p.key[p.passes & 1];
   const int32_t* pos = p.pos[p.passes & 1];
@@ -258,14 +258,14 @@ __global__ __launch_bounds__(256) void k_embed_runs(EmbedGradParams p, int cl) {
   flush(i1 < p.T && key[i1] == cur);
 }
 
-constexpr int kJoin = 512;
+constexpr int kJoin = 512, kJoinLanes = 4;
 // Rows whose runs cross chunks: the workgroup of the chunk in which a run
 // begins sums its parts, kJoin / 2^cl groups of lanes taking every so many
 // chunks, and then the groups' sums in order.
 template <int VEC, bool WHOLE>
 __global__ __launch_bounds__(kJoin) void k_embed_join(EmbedGradParams p, int cl) {
   __shared__ float sums[kJoin * VEC];
-  const int64_t chunk = blockIdx.x, i0 = chunk * kEmbedChunk, i1 = i0 + kEmbedChunk;
+  const int64_t chunk = blockIdx.x, i0 = chunk * p.chunk, i1 = i0 + p.chunk;
   if (i1 >= p.T) return;
   const uint32_t* key = p.key[p.passes & 1];
   const uint32_t cur = key[i1 - 1];
@@ -278,13 +278,13 @@ __global__ __launch_bounds__(kJoin) void k_embed_join(EmbedGradParams p, int cl)
   if (col < p.C) {
     if (lr == 0) load_n<float, VEC, WHOLE>(p.part + (2 * chunk + 1) * p.C, col, p.C, s);
     constexpr int AHEAD = 4;
-    for (int64_t q = chunk + 1 + lr; q * kEmbedChunk < p.T && key[q * kEmbedChunk] == cur; q += AHEAD * rl) {
+    for (int64_t q = chunk + 1 + lr; q * p.chunk < p.T && key[q * p.chunk] == cur; q += AHEAD * rl) {
       float v[AHEAD][VEC];
       bool in[AHEAD];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         const int64_t at = q + u * rl;
-        in[u] = at * kEmbedChunk < p.T && key[at * kEmbedChunk] == cur;
+        in[u] = at * p.chunk < p.T && key[at * p.chunk] == cur;
         if (in[u]) load_n<float, VEC, WHOLE>(p.part + 2 * at * p.C, col, p.C, v[u]);
       }
 #pragma unroll
@@ -387,11 +387,16 @@ __global__ __launch_bounds__(256) void k_embed_few(EmbedGradParams p, int cl) {
 
 template <typename T, int VEC, bool WHOLE>
 void embed_sums(const EmbedGradParams& p, hipStream_t s) {
-  const int64_t lanes = (p.C + VEC - 1) / VEC, chunks = (p.T + kEmbedChunk - 1) / kEmbedChunk;
+  const int64_t lanes = (p.C + VEC - 1) / VEC, chunks = (p.T + p.chunk - 1) / p.chunk;
   const int cl = pow2_log2(lanes, 6);
   const unsigned strips = (unsigned)((lanes + (1 << cl) - 1) >> cl), per = 256u >> cl;
   k_embed_runs<T, VEC, WHOLE><<<dim3((unsigned)((chunks + per - 1) / per), strips), 256, 0, s>>>(p, cl);
-  if (chunks > 1) k_embed_join<VEC, WHOLE><<<dim3((unsigned)(chunks - 1), strips), kJoin, 0, s>>>(p, cl);
+  if (chunks > 1) {
+    // narrow strips: one symbol may have every chunk, and its parts are then
+    // joined by a single workgroup per strip
+    const int jl = std::min(cl, kJoinLanes);
+    k_embed_join<VEC, WHOLE><<<dim3((unsigned)(chunks - 1), (unsigned)((lanes + (1 << jl) - 1) >> jl)), kJoin, 0, s>>>(p, jl);
+  }
 }
 
 }  // namespace

@@ -45,7 +45,7 @@ template <typename T> hipError_t launch_lin_pair(const LinGemmParams& dx, const 
 // wide) whose weights fit the LDS.
 constexpr size_t kLinRowsLds = 160 * 1024;
 size_t lin_rows_lds(int elem_bytes, int strip, int64_t K);
-int lin_rows_strip(int prod, int elem_bytes, int64_t Q, int64_t K);
+int lin_rows_strip(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K);
 template <typename T>
 hipError_t launch_lin_rows(const LinGemmParams&, int prod, int strip, hipStream_t);
 
@@ -100,13 +100,18 @@ struct EmbedGradParams {
   int32_t* counts; int32_t* totals;
   float* part;  // [chunks][2][C]: the sums of runs that cross a chunk's start, end
   int passes, bits;
+  int chunk;  // sorted positions summed by one group of lanes
 };
 constexpr int kEmbedFew = 2048;   // positions up to which no sort is needed
 // positions of a workgroup of the sort: small ones until they would make more
 // workgroups than the card takes at once
 constexpr int kEmbedTileSmall = 512, kEmbedTile = 2048;
 constexpr int embed_tile(int64_t T) { return T <= (1 << 18) ? kEmbedTileSmall : kEmbedTile; }
-constexpr int kEmbedChunk = 64;   // sorted positions summed by one group of lanes
+// Sorted positions summed by one group of lanes: few, so that there are waves
+// enough, while joining the parts of long runs costs little.  Chunks of 16 / 32 /
+// 64 / 128: 16,384 positions x 512 25 / 26 / 30 us; 65,536 x 256 (words) 54 / 53 / 59;
+// 131,072 x 128 (256 symbols) 41 / 38 / 36 / 41; 1,048,576 x 128 188 / 145 / 123 / 112.
+constexpr int embed_chunk(int64_t T) { return T < (1 << 15) ? 16 : T < (1 << 17) ? 32 : T <= (1 << 19) ? 64 : 128; }
 template <typename T> hipError_t launch_embed_grad(const EmbedGradParams&, hipStream_t);
 
 // ---- optimiser ------------------------------------------------------------------

@@ -125,7 +125,7 @@ LinPlan lin_plan(int prod, int bs, int64_t P, int64_t Q, int64_t K) {
   const int64_t bk = lin_step(bs), steps = cdiv(K, bk);
   const bool weight = prod == kLinWeight;
   pl.splits = 1;
-  if (P >= kLinRowsFrom) pl.strip = lin_rows_strip(prod, bs, Q, K);
+  if (P >= kLinRowsFrom) pl.strip = lin_rows_strip(prod, bs, P, Q, K);
   if (pl.strip) return pl;
   int64_t bp, bq;
   if (Q <= 32 && P > 64) { pl.tile = kTile128x32; bp = 128; bq = 32; }
@@ -293,7 +293,8 @@ size_t embed_ws(EmbedGradParams& p, void* base) {
   p.passes = (bits + 9) / 10;
   p.bits = (bits + p.passes - 1) / p.passes;
   if (p.T <= kEmbedFew) return 0;
-  const int64_t nb = cdiv(p.T, embed_tile(p.T)), chunks = cdiv(p.T, kEmbedChunk);
+  p.chunk = embed_chunk(p.T);
+  const int64_t nb = cdiv(p.T, embed_tile(p.T)), chunks = cdiv(p.T, p.chunk);
   Carver cv{static_cast<char*>(base)};
   for (int i = 0; i < 2; ++i) {
     p.key[i] = static_cast<uint32_t*>(cv.take(4 * p.T));

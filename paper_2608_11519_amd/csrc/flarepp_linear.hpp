@@ -220,41 +220,51 @@ template <typename T> __device__ __forceinline__ void row_vectors(const f32x16& 
     for (int u = 0; u < 4; ++u) q[u] = f32x4{v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]};
   }
 }
+// The 32 values of a row of the residual that go with a block, in its layout
+// (element 4 u + e: column 8 u + 4 g + e), read 16 bytes per lane
+template <typename T> struct ResBlock {
+  f32x4 v[sizeof(T)];
+  __device__ __forceinline__ void load(const T* row) {
+    const int g = lane_id() >> 5;
+#pragma unroll
+    for (int u = 0; u < (int)sizeof(T); ++u)
+      v[u] = *reinterpret_cast<const f32x4*>(row + (sizeof(T) == 2 ? 16 * u + 8 * g : 8 * u + 4 * g));
+  }
+  __device__ __forceinline__ void add_to(f32x16& y) const {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 w = runs_of_8(__builtin_bit_cast(bf16x8, v[u]));  // (its own inverse)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[8 * u + e] += (float)w[e];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] += v[e / 4][e % 4];
+    }
+  }
+};
 // One 32 x 32 block of C inside the row (Q % EPC == 0): lane (c, g) holds row c,
 // outputs 8 u + 4 g .. + 3 of the block in y[4 u ..].  res, out and pre point to
-// the row's first output of the block (or are null); bias(u) gives the four
-// biases of run u.  Stores of 16 bytes per lane.
+// the row's first output of the block (or are null); bias adds to a block.
+// Stores of 16 bytes per lane.
 template <typename T, int ACT, typename Bias>
 __device__ __forceinline__ void epilogue_whole(f32x16 y, const T* res, T* out, T* pre, bool in, Bias bias) {
   const int g = lane_id() >> 5;
-  typename Frag<T>::half r[4];
-  if (res) {
-#pragma unroll
-    for (int u = 0; u < 4; ++u) r[u] = load_half(res + 8 * u + 4 * g);
-  }
+  ResBlock<T> r;
+  if (res) r.load(res);
   bias(y);
   auto put = [&](T* d, const f32x16& v) __attribute__((always_inline)) {
+    f32x4 q[sizeof(T)];
+    row_vectors<T>(v, q);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if constexpr (sizeof(T) == 2) {
-        bf16x8 w;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = (__bf16)v[8 * u + e];
-        w = runs_of_8(w);
-        if (in) *reinterpret_cast<bf16x8*>(d + 16 * u + 8 * g) = w;
-      } else if (in) {
-        store4(d + 16 * u + 4 * g, v[8 * u], v[8 * u + 1], v[8 * u + 2], v[8 * u + 3]);
-        store4(d + 16 * u + 8 + 4 * g, v[8 * u + 4], v[8 * u + 5], v[8 * u + 6], v[8 * u + 7]);
-      }
-    }
+    for (int m = 0; m < (int)sizeof(T); ++m)
+      if (in) *reinterpret_cast<f32x4*>(d + (2 * m + g) * (16 / (int)sizeof(T))) = q[m];
   };
   if (pre) put(pre, y);
 #pragma unroll
   for (int e = 0; e < 16; ++e) y[e] = activate<ACT>(y[e]);
-  if (res) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) y[e] += to_f32(r[e / 4][e % 4]);
-  }
+  if (res) r.add_to(y);
   put(out, y);
 }
 // the same for rows of any width and blocks that pass the row's end

@@ -142,7 +142,7 @@ __global__ __launch_bounds__(512, rows_waves(NB, sizeof(T))) void k_linear_rows(
       const int64_t row = tile * 32 + c;
       if constexpr (WHOLE) {
         const int64_t at = min(row, p.P - 1) * p.Q + q0;
-        const T* res = p.res ? static_cast<const T*>(p.res) + at + 4 * g : nullptr;
+        const T* res = p.res ? static_cast<const T*>(p.res) + at : nullptr;
         const int64_t first = scalar64(tile * 32 * p.Q + q0);
         const int rows = (int)min((int64_t)32, p.P - tile * 32);
         constexpr int NG = sizeof(T) == 2 && NB >= 64 ? 2 : 1;  // blocks stored together
@@ -157,12 +157,9 @@ __global__ __launch_bounds__(512, rows_waves(NB, sizeof(T))) void k_linear_rows(
           for (int d = 0; d < NG; ++d) {
             const int i = i0 + d;
             f32x16 v = acc[i];
-            typename Frag<T>::half r[4];
+            ResBlock<T> r;
             const bool inside = q0 + 32 * i < p.Q;  // uniform
-            if (res && inside) {
-#pragma unroll
-              for (int u = 0; u < 4; ++u) r[u] = load_half(res + 32 * i + 8 * u);
-            }
+            if (res && inside) r.load(res + 32 * i);
             if (p.bias) {
 #pragma unroll
               for (int u = 0; u < 4; ++u) {
@@ -176,10 +173,7 @@ __global__ __launch_bounds__(512, rows_waves(NB, sizeof(T))) void k_linear_rows(
 #pragma unroll
               for (int e = 0; e < 16; ++e) v[e] = activate<decltype(act)::value>(v[e]);
             });
-            if (res && inside) {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) v[e] += to_f32(r[e / 4][e % 4]);
-            }
+            if (res && inside) r.add_to(v);
             row_vectors<T>(v, &o[d * sizeof(T)]);
           }
           store_rows<NV>(region, o, static_cast<T*>(p.out) + first + 32 * i0, (uint32_t)(p.Q * sizeof(T)), rows, vectors);
@@ -242,15 +236,16 @@ size_t lin_rows_lds(int elem_bytes, int strip, int64_t K) {
 // are whole steps, or short; outputs that are whole blocks, or (forward) few;
 // weights that fit; and L read at most twice.  Rows / tiles: 131,072 x 256 -> 128
 // 29 / 37 us, 100,000 x 256 -> 512 (two strips) 78 / 85, 200,000 x 512 -> 128 82 / 101;
-// beyond, 200,000 x 1024 -> 64 114 / 98, 100,000 x 512 -> 256 (two strips) 63 / 56.
-int lin_rows_strip(int prod, int elem_bytes, int64_t Q, int64_t K) {
+// beyond, 200,000 x 1024 -> 64 114 / 98; 512 -> 256 (two strips) with residual, 30,000 rows
+// 25 / 18, 100,000 73 / 69, 200,000 118 / 129, 400,000 197 / 231.
+int lin_rows_strip(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K) {
   const bool whole = Q % 32 == 0, steps = K % 16 == 0;
   if (prod == kLinWeight || K > 512 || (!steps && (K > 32 || !whole)) || (!whole && (prod != kLinForward || Q > 64))) return 0;
   const int widest = elem_bytes == 2 ? 256 : 64;
   int strip = 32;
   while (strip < widest && strip < Q) strip *= 2;
   while (strip > 32 && lin_rows_lds(elem_bytes, strip, K) > kLinRowsLds) strip /= 2;
-  return lin_rows_lds(elem_bytes, strip, K) <= kLinRowsLds && (Q + strip - 1) / strip <= (K < 512 ? 2 : 1) ? strip : 0;
+  return lin_rows_lds(elem_bytes, strip, K) <= kLinRowsLds && (Q + strip - 1) / strip <= (K < 512 || P >= (1 << 17) ? 2 : 1) ? strip : 0;
 }
 
 template <typename T>
