@@ -208,6 +208,30 @@ __device__ __forceinline__ void linear_tile(const LinGemmParams& p, int block, c
     }
   }
 
+  if (!p.part && p.Q % EPC == 0) {
+    // whole vectors: rows go out through LDS, which every wave has left
+    __syncthreads();
+    char* region = smem + wave * 2048;
+    constexpr int NG = sizeof(T) == 2 && NQ % 2 == 0 ? 2 : 1;
+    static_for<0, NP>([&](auto jc) __attribute__((always_inline)) {
+      constexpr int j = decltype(jc)::value;
+      const int64_t row0 = scalar64(p0 + 32 * (wp * NP + j));
+      if (row0 >= p.P) return;
+      static_for<0, NQ / NG>([&](auto ic) __attribute__((always_inline)) {
+        constexpr int i0 = decltype(ic)::value * NG;
+        const int64_t qb = scalar64(q0 + 32 * (wq * NQ + i0));
+        if (qb >= p.Q) return;
+        f32x16 v[NG];
+#pragma unroll
+        for (int d = 0; d < NG; ++d) v[d] = acc[i0 + d][j];
+        epilogue_group<T, NG>(v, p, region, row0, qb, [&](int u) __attribute__((always_inline)) {
+          const auto b = load_half(static_cast<const T*>(p.bias) + min(qb + 8 * u + 4 * g, p.Q - 4));
+          return f32x4{to_f32(b[0]), to_f32(b[1]), to_f32(b[2]), to_f32(b[3])};
+        });
+      });
+    });
+    return;
+  }
   static_for<0, NP>([&](auto jc) __attribute__((always_inline)) {
     constexpr int j = decltype(jc)::value;
     const int64_t row = p0 + 32 * (wp * NP + j) + c;
@@ -216,25 +240,7 @@ __device__ __forceinline__ void linear_tile(const LinGemmParams& p, int block, c
       const int64_t qb = q0 + 32 * (wq * NQ + i);
       if (qb >= p.Q) return;
       if (!p.part) {
-        if (p.Q % EPC == 0 && qb + 32 <= p.Q) {
-          const int64_t at = min(row, p.P - 1) * p.Q + qb;
-          auto bias = [&](f32x16& y) __attribute__((always_inline)) {
-            if (!p.bias) return;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const auto v = load_half(static_cast<const T*>(p.bias) + qb + 8 * u + 4 * g);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) y[4 * u + e] += to_f32(v[e]);
-            }
-          };
-          with_act(p.act, [&](auto act) __attribute__((always_inline)) {
-            epilogue_whole<T, decltype(act)::value>(acc[i][j], p.res ? static_cast<const T*>(p.res) + at : nullptr,
-                                                    static_cast<T*>(p.out) + at, p.pre ? static_cast<T*>(p.pre) + at : nullptr,
-                                                    row < p.P, bias);
-          });
-        } else {
-          epilogue_parts<T>(acc[i][j], p, row, qb);
-        }
+        epilogue_parts<T>(acc[i][j], p, row, qb);
         return;
       }
       const bool whole = p.Q % 4 == 0;

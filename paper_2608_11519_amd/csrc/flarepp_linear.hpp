@@ -230,6 +230,16 @@ template <typename T> struct ResBlock {
     for (int u = 0; u < (int)sizeof(T); ++u)
       v[u] = *reinterpret_cast<const f32x4*>(row + (sizeof(T) == 2 ? 16 * u + 8 * g : 8 * u + 4 * g));
   }
+  // the same where the row ends after `left` columns (a multiple of a vector, maybe none)
+  __device__ __forceinline__ void load_cut(const T* row, int left) {
+    const int g = lane_id() >> 5;
+#pragma unroll
+    for (int u = 0; u < (int)sizeof(T); ++u) {
+      const int col = sizeof(T) == 2 ? 16 * u + 8 * g : 8 * u + 4 * g;
+      v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (col < left) v[u] = *reinterpret_cast<const f32x4*>(row + col);
+    }
+  }
   __device__ __forceinline__ void add_to(f32x16& y) const {
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -244,28 +254,75 @@ template <typename T> struct ResBlock {
     }
   }
 };
-// One 32 x 32 block of C inside the row (Q % EPC == 0): lane (c, g) holds row c,
-// outputs 8 u + 4 g .. + 3 of the block in y[4 u ..].  res, out and pre point to
-// the row's first output of the block (or are null); bias adds to a block.
-// Stores of 16 bytes per lane.
-template <typename T, int ACT, typename Bias>
-__device__ __forceinline__ void epilogue_whole(f32x16 y, const T* res, T* out, T* pre, bool in, Bias bias) {
-  const int g = lane_id() >> 5;
-  ResBlock<T> r;
-  if (res) r.load(res);
-  bias(y);
-  auto put = [&](T* d, const f32x16& v) __attribute__((always_inline)) {
-    f32x4 q[sizeof(T)];
-    row_vectors<T>(v, q);
+// Stores NV * 32 bytes (the first `vectors` 16-byte ones) of each of a tile's 32 rows: lane (c, g) holds row c, 16-byte
+// vectors 2 m + g in q[m].  Through 2 KiB of the wave's LDS, 16 rows at a time, so
+// that an instruction stores whole 64- or 128-byte runs of its rows: straight from
+// the product's layout (32 bytes of 32 rows) part of the lines are written twice
+// (131,072 x 128 -> 256 with pre: 161 MB for 134; GELU 56 us, 46 so; 1,048,576 x 128 -> 128
+// with residual 209, 160).
+template <int NV>
+__device__ __forceinline__ void store_rows(char* region, const f32x4 (&q)[NV], void* dst, uint32_t row_bytes, int rows,
+                                           int vectors) {
+  const int lane = lane_id(), g = lane >> 5, c = lane & 31;
+  constexpr int RB = NV * 32, PER = 64 / (2 * NV);  // bytes of a row, rows of an instruction
+  auto slot = [](int row, int v) __attribute__((always_inline)) { return v ^ (row / (256 / RB) & (2 * NV - 1)); };
 #pragma unroll
-    for (int m = 0; m < (int)sizeof(T); ++m)
-      if (in) *reinterpret_cast<f32x4*>(d + (2 * m + g) * (16 / (int)sizeof(T))) = q[m];
-  };
-  if (pre) put(pre, y);
+  for (int h = 0; h < 2; ++h) {
+    if ((c >> 4) == h) {
 #pragma unroll
-  for (int e = 0; e < 16; ++e) y[e] = activate<ACT>(y[e]);
-  if (res) r.add_to(y);
-  put(out, y);
+      for (int m = 0; m < NV; ++m) *reinterpret_cast<f32x4*>(region + (c & 15) * RB + slot(c & 15, 2 * m + g) * 16) = q[m];
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 16 / PER; ++j) {
+      const int r = j * PER + lane / (2 * NV), v = lane % (2 * NV);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(region + r * RB + slot(r, v) * 16);
+      const int row = 16 * h + r;
+      if (row < rows && v < vectors) *reinterpret_cast<f32x4*>(static_cast<char*>(dst) + (uint32_t)row * row_bytes + v * 16) = x;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Bias, activation, residual and stores of NG 32 x 32 blocks of C side by side,
+// rows row0 .., outputs q .. (Q whole 16-byte vectors; vectors past the row's end
+// are not stored): lane (c, g) holds row c, outputs 8 u + 4 g .. + 3 of a block in
+// v[4 u ..]; bias(u) gives the four biases of run u of all blocks.
+template <typename T, int NG, typename Bias>
+__device__ __forceinline__ void epilogue_group(f32x16 (&v)[NG], const LinGemmParams& p, char* region, int64_t row0, int64_t q,
+                                               Bias bias) {
+  constexpr int ES = sizeof(T), NV = NG * ES;  // 16-byte vectors of a row per lane
+  const int c = lane_id() & 31;
+  const int rows = (int)min((int64_t)32, p.P - row0), vectors = (int)min((int64_t)2 * NV, (p.Q - q) * ES / 16);
+  const int64_t first = row0 * p.Q + q;
+  f32x4 o[NV], y[NV];
+#pragma unroll
+  for (int d = 0; d < NG; ++d) {
+    ResBlock<T> r;
+    const bool inside = q + 32 * d + 32 <= p.Q;  // uniform; a cut block's residual is read by vectors
+    if (p.res) {
+      const T* at = static_cast<const T*>(p.res) + first + (int64_t)min(c, rows - 1) * p.Q + 32 * d;
+      if (inside) r.load(at);
+      else r.load_cut(at, (int)(p.Q - q) - 32 * d);
+    }
+    if (p.bias) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const f32x4 b = bias(4 * d + u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[d][4 * u + e] += b[e];
+      }
+    }
+    if (p.pre) row_vectors<T>(v[d], &y[d * ES]);
+    with_act(p.act, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[d][e] = activate<decltype(act)::value>(v[d][e]);
+    });
+    if (p.res) r.add_to(v[d]);
+    row_vectors<T>(v[d], &o[d * ES]);
+  }
+  store_rows<NV>(region, o, static_cast<T*>(p.out) + first, (uint32_t)(p.Q * ES), rows, vectors);
+  if (p.pre) store_rows<NV>(region, y, static_cast<T*>(p.pre) + first, (uint32_t)(p.Q * ES), rows, vectors);
 }
 // the same for rows of any width and blocks that pass the row's end
 template <typename T>

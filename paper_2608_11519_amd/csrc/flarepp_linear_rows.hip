@@ -13,36 +13,6 @@ namespace {
 // follows the weights' copy.
 // STEPS: K is whole steps of 16 (else rows are read by single elements).
 // WHOLE: Q is whole blocks of 32.
-// Stores NV * 32 bytes (the first `vectors` 16-byte ones) of each of a tile's 32 rows: lane (c, g) holds row c, 16-byte
-// vectors 2 m + g in q[m].  Through 2 KiB of the wave's LDS, 16 rows at a time, so
-// that an instruction stores whole 64- or 128-byte runs of its rows: straight from
-// the product's layout (32 bytes of 32 rows) part of the lines are written twice
-// (131,072 x 128 -> 256 with pre: 161 MB for 134; GELU 56 us, 46 so; 1,048,576 x 128 -> 128
-// with residual 209, 160).
-template <int NV>
-__device__ __forceinline__ void store_rows(char* region, const f32x4 (&q)[NV], void* dst, uint32_t row_bytes, int rows,
-                                           int vectors) {
-  const int lane = lane_id(), g = lane >> 5, c = lane & 31;
-  constexpr int RB = NV * 32, PER = 64 / (2 * NV);  // bytes of a row, rows of an instruction
-  auto slot = [](int row, int v) __attribute__((always_inline)) { return v ^ (row / (256 / RB) & (2 * NV - 1)); };
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if ((c >> 4) == h) {
-#pragma unroll
-      for (int m = 0; m < NV; ++m) *reinterpret_cast<f32x4*>(region + (c & 15) * RB + slot(c & 15, 2 * m + g) * 16) = q[m];
-    }
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int j = 0; j < 16 / PER; ++j) {
-      const int r = j * PER + lane / (2 * NV), v = lane % (2 * NV);
-      const f32x4 x = *reinterpret_cast<const f32x4*>(region + r * RB + slot(r, v) * 16);
-      const int row = 16 * h + r;
-      if (row < rows && v < vectors) *reinterpret_cast<f32x4*>(static_cast<char*>(dst) + (uint32_t)row * row_bytes + v * 16) = x;
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
-}
-
 // Waves per SIMD: four for the narrowest strip (500,000 x 64 -> 4 25 -> 21 us), two
 // for the others, whose loads ahead are worth more than the waves (1,048,576 x
 // 64 -> 64 101 us, 115 with four; 200,000 x 512 -> 128 82, 109).
@@ -141,44 +111,18 @@ __global__ __launch_bounds__(512, rows_waves(NB, sizeof(T))) void k_linear_rows(
     if (last) {
       const int64_t row = tile * 32 + c;
       if constexpr (WHOLE) {
-        const int64_t at = min(row, p.P - 1) * p.Q + q0;
-        const T* res = p.res ? static_cast<const T*>(p.res) + at : nullptr;
-        const int64_t first = scalar64(tile * 32 * p.Q + q0);
-        const int rows = (int)min((int64_t)32, p.P - tile * 32);
         constexpr int NG = sizeof(T) == 2 && NB >= 64 ? 2 : 1;  // blocks stored together
-        constexpr int NV = NG * (int)sizeof(T);                  // 16-byte vectors of a row per lane
         char* region = smem + nbuf * R::BYTES + NB * sizeof(float) + wave * 2048;
+        static_for<0, NQ / NG>([&](auto ic) __attribute__((always_inline)) {
+          constexpr int i0 = decltype(ic)::value * NG;
+          if (q0 + 32 * i0 >= p.Q) return;
+          f32x16 v[NG];
 #pragma unroll
-        for (int i0 = 0; i0 < NQ; i0 += NG) {
-          if (q0 + 32 * i0 >= p.Q) continue;
-          f32x4 o[NV], y[NV];
-          const int vectors = (int)min((int64_t)2 * NV, (p.Q - q0 - 32 * i0) / EPC);
-#pragma unroll
-          for (int d = 0; d < NG; ++d) {
-            const int i = i0 + d;
-            f32x16 v = acc[i];
-            ResBlock<T> r;
-            const bool inside = q0 + 32 * i < p.Q;  // uniform
-            if (res && inside) r.load(res + 32 * i);
-            if (p.bias) {
-#pragma unroll
-              for (int u = 0; u < 4; ++u) {
-                const f32x4 bv = *reinterpret_cast<const f32x4*>(lbias + 32 * i + 8 * u + 4 * g);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[4 * u + e] += bv[e];
-              }
-            }
-            if (p.pre) row_vectors<T>(v, &y[d * sizeof(T)]);
-            with_act(p.act, [&](auto act) __attribute__((always_inline)) {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) v[e] = activate<decltype(act)::value>(v[e]);
-            });
-            if (res && inside) r.add_to(v);
-            row_vectors<T>(v, &o[d * sizeof(T)]);
-          }
-          store_rows<NV>(region, o, static_cast<T*>(p.out) + first + 32 * i0, (uint32_t)(p.Q * sizeof(T)), rows, vectors);
-          if (p.pre) store_rows<NV>(region, y, static_cast<T*>(p.pre) + first + 32 * i0, (uint32_t)(p.Q * sizeof(T)), rows, vectors);
-        }
+          for (int d = 0; d < NG; ++d) v[d] = acc[i0 + d];
+          epilogue_group<T, NG>(v, p, region, scalar64(tile * 32), q0 + 32 * i0, [&](int u) __attribute__((always_inline)) {
+            return *reinterpret_cast<const f32x4*>(lbias + 32 * i0 + 8 * u + 4 * g);
+          });
+        });
       } else {
 #pragma unroll
         for (int i = 0; i < NQ; ++i)
