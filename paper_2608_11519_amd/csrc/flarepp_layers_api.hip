@@ -118,9 +118,8 @@ struct LinPlan {
 // Tile by the product's shape: narrow ones (at most 32 outputs or rows) take a
 // narrow tile, others 128 x 128 where these give every CU a workgroup, else
 // 64 x 64.  The weight gradient, whose tokens can be split, takes 128 x 128 from
-// 8192 tokens or that much work on (128 x 128 / 64 x 64: 4096 tokens, 2048 x 2048 53 / 84
-// us, 1024 x 1024 34 / 26; 8000, 1000 x 1000 40 / 47); below, 64 x 64 tiles let both
-// products of a backward go in one launch.  A reduction is
+// 8192 tokens or 17 tiles on (4096 x 2048 x 2048 53 us, 84 in 64 x 64 tiles); below,
+// 64 x 64 tiles let both products of a backward go in one launch.  A reduction is
 // split when the tiles alone would leave CUs idle: the weight gradient's, or that
 // of a forward or input-gradient product of eight steps or more (fewer cost less
 // than the second launch).
@@ -134,7 +133,7 @@ LinPlan lin_plan(int prod, int bs, int64_t P, int64_t Q, int64_t K) {
   int64_t bp, bq;
   if (Q <= 32 && P > 64) { pl.tile = kTile128x32; bp = 128; bq = 32; }
   else if (P <= 32 && Q > 64) { pl.tile = kTile32x128; bp = 32; bq = 128; }
-  else if (P > 64 && Q > 64 && (weight ? K >= kLinRowsFrom || cdiv(P, 128) * cdiv(Q, 128) * K > (1 << 18)
+  else if (P > 64 && Q > 64 && (weight ? K >= kLinRowsFrom || cdiv(P, 128) * cdiv(Q, 128) > 16
                                         : cdiv(P, 128) * cdiv(Q, 128) >= 256)) { pl.tile = kTile128; bp = bq = 128; }
   else { pl.tile = kTile64; bp = bq = 64; }
   if (pl.tile == kTile128 && !weight && bs == 2 && lin_direct(prod, bs, P, Q, K)) {
