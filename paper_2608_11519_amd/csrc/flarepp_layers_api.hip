@@ -117,9 +117,13 @@ struct LinPlan {
 
 // Tile by the product's shape: narrow ones (at most 32 outputs or rows) take a
 // narrow tile, others 128 x 128 where these give every CU a workgroup, else
-// 64 x 64.  The weight gradient, whose tokens can be split, takes 128 x 128 from
-// 8192 tokens or 17 tiles on (4096 x 2048 x 2048 53 us, 84 in 64 x 64 tiles); below,
-// 64 x 64 tiles let both products of a backward go in one launch.  A reduction is
+// 64 x 64.  The weight gradient, whose tokens can be split, takes 128 x 128 where
+// its tiles times tokens times bytes of an element pass 2^19, else 64 x 64, which split
+// finer and let both products of a backward go in one launch.  Both products, 128 x 128 /
+// 64 x 64, us: bf16 2000 x 1000 x 1000 44 / 30, 16,384 x 512 x 512 44 / 42, 4096 x 1024 x
+// 1024 48 / 46, 8000 x 1000 x 1000 67 / 76, 4096 x 2048 x 2048 93 / 126; fp32 2000 x 1000 x
+// 1000 96 / 82, 60,969 x 128 x 256 104 / 100, 8000 x 512 x 640 118 / 121, 8000 x 1000 x 1000
+// 278 / 324; off at fp32 21,668 x 274 x 459 (212 / 190).  A reduction is
 // split when the tiles alone would leave CUs idle: the weight gradient's, or that
 // of a forward or input-gradient product of eight steps or more (fewer cost less
 // than the second launch).
@@ -133,7 +137,7 @@ LinPlan lin_plan(int prod, int bs, int64_t P, int64_t Q, int64_t K) {
   int64_t bp, bq;
   if (Q <= 32 && P > 64) { pl.tile = kTile128x32; bp = 128; bq = 32; }
   else if (P <= 32 && Q > 64) { pl.tile = kTile32x128; bp = 32; bq = 128; }
-  else if (P > 64 && Q > 64 && (weight ? K >= kLinRowsFrom || cdiv(P, 128) * cdiv(Q, 128) > 16
+  else if (P > 64 && Q > 64 && (weight ? cdiv(P, 128) * cdiv(Q, 128) * K * bs > (1 << 19)
                                         : cdiv(P, 128) * cdiv(Q, 128) >= 256)) { pl.tile = kTile128; bp = bq = 128; }
   else { pl.tile = kTile64; bp = bq = 64; }
   if (pl.tile == kTile128 && !weight && bs == 2 && lin_direct(prod, bs, P, Q, K)) {
