@@ -92,10 +92,12 @@ __device__ __forceinline__ void clear_slice(float* p, int64_t n) {
   const int64_t tail = n / 4 * 4 + threadIdx.x;
   if (blockIdx.x == 0 && tail < n) p[tail] = 0.f;
 }
+int clear_groups(int64_t n) { return (int)std::min<int64_t>(2048, (n + 1023) / 1024); }
 __global__ __launch_bounds__(256) void k_embed_clear(float* p, int64_t n) { clear_slice(p, n); }
 
 // counts[digit][workgroup] of tiles of TILE positions; the first pass also
-// clears the table's gradient
+// clears the table's gradient, by workgroups past the nb of the positions where
+// these are few
 template <int TILE>
 __global__ __launch_bounds__(256) void k_embed_count(EmbedGradParams p, int pass, int nb) {
   __shared__ int hist[1024];
@@ -109,6 +111,7 @@ __global__ __launch_bounds__(256) void k_embed_count(EmbedGradParams p, int pass
     if (i < p.T) atomicAdd(&hist[embed_key(p, pass, i) >> shift & (bins - 1)], 1);
   }
   if (pass == 0) clear_slice(p.dtable, p.V * p.C);
+  if ((int)blockIdx.x >= nb) return;  // whole workgroup
   __syncthreads();
   for (int b = threadIdx.x; b < bins; b += 256) p.counts[(int64_t)b * nb + blockIdx.x] = hist[b];
 }
@@ -416,7 +419,7 @@ template hipError_t launch_embed<float>(const EmbedParams&, hipStream_t);
 template hipError_t launch_embed<__bf16>(const EmbedParams&, hipStream_t);
 
 template <typename T, int VEC, bool WHOLE>
-void embed_few(const EmbedGradParams& p, hipStream_t s) {
+void embed_unsorted(const EmbedGradParams& p, hipStream_t s) {
   const int64_t lanes = (p.C + VEC - 1) / VEC;
   const int cl = pow2_log2(lanes, 5);  // eight groups at least: one symbol may have every position
   k_embed_few<T, VEC, WHOLE><<<dim3((unsigned)p.T, (unsigned)((lanes + (1 << cl) - 1) >> cl)), 256, 0, s>>>(p, cl);
@@ -424,7 +427,7 @@ void embed_few(const EmbedGradParams& p, hipStream_t s) {
 template <int TILE> void embed_sort(const EmbedGradParams& p, hipStream_t s) {
   const int nb = (int)((p.T + TILE - 1) / TILE);
   for (int pass = 0; pass < p.passes; ++pass) {
-    k_embed_count<TILE><<<dim3(nb), 256, 0, s>>>(p, pass, nb);
+    k_embed_count<TILE><<<dim3(pass ? nb : std::max(nb, clear_groups(p.V * p.C))), 256, 0, s>>>(p, pass, nb);
     k_embed_scan<<<dim3(1u << p.bits), 64, 0, s>>>(p, nb);
     k_embed_scatter<TILE><<<dim3(nb), 256, 0, s>>>(p, pass, nb);
   }
@@ -435,12 +438,12 @@ hipError_t launch_embed_grad(const EmbedGradParams& p, hipStream_t s) {
   // 16 bytes of a row of dOut per lane; the sums are stored as whole vectors too
   constexpr int V = 16 / (int)sizeof(T);
   const bool whole = p.C % V == 0, cut = p.C > V;
-  if (p.T <= kEmbedFew) {
+  if (embed_few(p.T, p.C)) {
     const int64_t n = p.V * p.C;
-    k_embed_clear<<<dim3((unsigned)std::min<int64_t>(2048, (n + 1023) / 1024)), 256, 0, s>>>(p.dtable, n);
-    if (whole) embed_few<T, V, true>(p, s);
-    else if (cut) embed_few<T, V, false>(p, s);
-    else embed_few<T, 1, true>(p, s);
+    k_embed_clear<<<dim3(clear_groups(n)), 256, 0, s>>>(p.dtable, n);
+    if (whole) embed_unsorted<T, V, true>(p, s);
+    else if (cut) embed_unsorted<T, V, false>(p, s);
+    else embed_unsorted<T, 1, true>(p, s);
     return hipGetLastError();
   }
   if (embed_tile(p.T) == kEmbedTileSmall) embed_sort<kEmbedTileSmall>(p, s);

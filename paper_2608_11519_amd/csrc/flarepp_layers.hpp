@@ -73,7 +73,7 @@ struct LinBwdParams {
   int64_t T, K, N, chunk;
   int nchunks, act;
 };
-bool lin_bwd_tile(int64_t K, int64_t N, int act, int& kt, int& nt, bool& fused);
+bool lin_bwd_tile(int64_t T, int64_t K, int64_t N, int act, int& kt, int& nt, bool& fused);
 hipError_t launch_lin_bwd(const LinBwdParams&, int kt, int nt, bool fused, hipStream_t);
 
 // out[i] = sum_s part[s * stride + i], i < n: two independent jobs in a launch
@@ -102,7 +102,12 @@ struct EmbedGradParams {
   int passes, bits;
   int chunk;  // sorted positions summed by one group of lanes
 };
-constexpr int kEmbedFew = 2048;   // positions up to which no sort is needed
+// Positions up to which no sort is needed: every position looks through all of
+// them, once per strip of columns, so up to 2048 and by T * T * C.  Unsorted /
+// sorted, us: 300 x 256 (30,000 symbols) 12 / 30; 2048 x 256 21 / 36, x 512 35 / 41, x 1024
+// 61 / 48; 1536 x 1024 47 / 47; 4096 x 128 (256 symbols) 35 / 20.
+constexpr int kEmbedFew = 2048;
+inline bool embed_few(int64_t T, int64_t C) { return T <= kEmbedFew && T * T * C <= int64_t(5) << 29; }
 // positions of a workgroup of the sort: small ones until they would make more
 // workgroups than the card takes at once
 constexpr int kEmbedTileSmall = 512, kEmbedTile = 2048;

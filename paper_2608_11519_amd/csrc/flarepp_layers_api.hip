@@ -105,8 +105,6 @@ int check_linear_shape(int dtype, int act, int64_t T, int64_t K, int64_t N) {
   return FLAREPP_OK;
 }
 
-constexpr int64_t kLinRowsFrom = 8192;  // rows from which the weights' copy into every CU pays
-
 struct LinPlan {
   int strip;  // not 0: k_linear_rows with strips of this width
   int tile, splits;
@@ -132,7 +130,7 @@ LinPlan lin_plan(int prod, int bs, int64_t P, int64_t Q, int64_t K) {
   const int64_t bk = lin_step(bs), steps = cdiv(K, bk);
   const bool weight = prod == kLinWeight;
   pl.splits = 1;
-  if (P >= kLinRowsFrom) pl.strip = lin_rows_strip(prod, bs, P, Q, K);
+  pl.strip = lin_rows_strip(prod, bs, P, Q, K);
   if (pl.strip) return pl;
   int64_t bp, bq;
   if (Q <= 32 && P > 64) { pl.tile = kTile128x32; bp = 128; bq = 32; }
@@ -179,9 +177,6 @@ int run_linear(int act, int64_t rows, int64_t K, int64_t N, const void* X, const
   return api_ok();
 }
 
-// From these tokens on the one-pass backward has chunks enough for every CU
-constexpr int64_t kLinBwdFrom = 8192;
-
 struct LinBwdWs {
   LinPlan dx, dw;
   bool pass, fused;  // one pass over the tokens; dX in it
@@ -205,7 +200,7 @@ LinBwdWs lin_bwd_ws(void* base, int dtype, int act, int64_t rows, int64_t K, int
   }
   // (few rows: one chunk, and no sum of partials)
   w.chunk = rows <= 128 ? rows : std::max<int64_t>(32, cdiv(rows, 512));
-  w.pass = dtype == FLAREPP_BF16 && rows >= kLinBwdFrom && lin_bwd_tile(K, N, act, w.kt, w.nt, w.fused);
+  w.pass = dtype == FLAREPP_BF16 && lin_bwd_tile(rows, K, N, act, w.kt, w.nt, w.fused);
   if (w.pass) {  // a workgroup per CU, of two steps at least
     const int64_t tiles = (K / w.kt) * (N / w.nt);
     const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, rows / 64));
@@ -300,7 +295,7 @@ size_t embed_ws(EmbedGradParams& p, void* base) {
   while ((int64_t(1) << bits) <= p.V) ++bits;  // symbols 0 .. V - 1, and V for padding
   p.passes = (bits + 9) / 10;
   p.bits = (bits + p.passes - 1) / p.passes;
-  if (p.T <= kEmbedFew) return 0;
+  if (embed_few(p.T, p.C)) return 0;
   p.chunk = embed_chunk(p.T);
   const int64_t nb = cdiv(p.T, embed_tile(p.T)), chunks = cdiv(p.T, p.chunk);
   Carver cv{static_cast<char*>(base)};

@@ -280,16 +280,19 @@ template <int KT, int NT> hipError_t launch_size(const LinBwdParams& p, bool fus
 
 // The tile of inputs and outputs (kt, nt) of the one-pass backward; fused: dX
 // too.  False where the products of k_linear take less time: sizes that are not
-// whole tiles, no activation (nothing is formed twice), or more than 256 inputs
-// (dP is formed again per tile of inputs).  100,000 tokens with GELU, one pass /
-// products: 256 x 512 186 / 227 us, 256 x 256 104 / 126, 512 x 256 184 / 183; 32,768
-// tokens, 512 x 1024 198 / 191; without activation 100,000 x 256 x 512 117 / 105.
-bool lin_bwd_tile(int64_t K, int64_t N, int act, int& kt, int& nt, bool& fused) {
+// whole tiles, tokens too few for their chunks' sums of dW, and, where dX is not
+// formed in the pass, no activation (nothing is formed twice) or more than 256
+// inputs (dP is formed again per tile of inputs).  One pass / products, us, GELU:
+// 64 x 64, 2048 tokens 8.4 / 10.7; 128 x 256, 8192 24 / 21, 16,384 25 / 27, 131,072 67 / 121;
+// 256 x 512, 24,576 50 / 58, 131,072 202 / 272; 256 x 256, 32,768 51 / 44, 49,152 60 / 68;
+// 512 x 128, 131,072 135 / 139; without activation 256 x 256, 131,072 102 / 99.
+bool lin_bwd_tile(int64_t T, int64_t K, int64_t N, int act, int& kt, int& nt, bool& fused) {
   auto ok = [](int64_t v) { return v == 64 || v == 128 || v == 256; };
   fused = ok(K) && ok(N) && K * N <= 128 * 256;
   kt = (int)K;
   nt = fused ? (int)N : 128;
-  return fused || (act != kActNone && (K == 128 || K == 256) && N % 128 == 0);
+  if (fused) return 2 * T >= K * N;
+  return act != kActNone && T >= (N > K ? 3 << 13 : 3 << 14) && (K == 128 || K == 256) && N % 128 == 0;
 }
 
 hipError_t launch_lin_bwd(const LinBwdParams& p, int kt, int nt, bool fused, hipStream_t s) {

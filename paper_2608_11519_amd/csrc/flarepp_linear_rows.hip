@@ -176,20 +176,24 @@ size_t lin_rows_lds(int elem_bytes, int strip, int64_t K) {
   return (size_t)((K + bk - 1) / bk) * strip * 128 + strip * sizeof(float) + 8 * 2048;  // weights, biases, stores
 }
 
-// The strip for a product, or 0 where another kernel has to do: rows of L that
-// are whole steps, or short; outputs that are whole blocks, or (forward) few;
-// weights that fit; and L read at most twice.  Rows / tiles: 131,072 x 256 -> 128
-// 29 / 37 us, 100,000 x 256 -> 512 (two strips) 78 / 85, 200,000 x 512 -> 128 82 / 101;
-// beyond, 200,000 x 1024 -> 64 114 / 98; 512 -> 256 (two strips) with residual, 30,000 rows
-// 25 / 18, 100,000 73 / 69, 200,000 118 / 129, 400,000 197 / 231.
+// The strip for a product, or 0 where the tiles take less time.  Weights that
+// every CU copies pay over many rows only: from 65,536 where the inputs or the
+// outputs are few (rows / tiles, us: fp32 4 -> 64, 32,768 rows 7.7 / 7.2, 65,536 8.5 / 11.9;
+// bf16 64 -> 3, 24,576 4.5 / 4.5, 65,536 5.2 / 5.6), and in bf16 from 98,304 to outputs
+// that are many and no fewer than the inputs, so that the stores are most of the
+// work (128 -> 256, 65,536 22 / 21, 100,000 35 / 37, 200,000 65 / 74; 256 -> 512, 65,536
+// 43 / 43, 200,000 133 / 150; not 256 -> 128, 200,000 48 / 47, nor fp32 256 -> 256, 257 / 257).
+// The kernel itself needs rows of L that are whole steps, or short; outputs that
+// are whole blocks, or (forward) few; weights that fit, and L read at most twice.
 int lin_rows_strip(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K) {
-  const bool whole = Q % 32 == 0, steps = K % 16 == 0;
+  const bool whole = Q % 32 == 0, steps = K % 16 == 0, few = K <= 32 || Q <= 32;
+  if (few ? P < (1 << 16) : elem_bytes != 2 || P < (3 << 15) || Q < 256 || Q < K) return 0;
   if (prod == kLinWeight || K > 512 || (!steps && (K > 32 || !whole)) || (!whole && (prod != kLinForward || Q > 64))) return 0;
   const int widest = elem_bytes == 2 ? 256 : 64;
   int strip = 32;
   while (strip < widest && strip < Q) strip *= 2;
   while (strip > 32 && lin_rows_lds(elem_bytes, strip, K) > kLinRowsLds) strip /= 2;
-  return lin_rows_lds(elem_bytes, strip, K) <= kLinRowsLds && (Q + strip - 1) / strip <= (K < 512 || P >= (1 << 17) ? 2 : 1) ? strip : 0;
+  return lin_rows_lds(elem_bytes, strip, K) <= kLinRowsLds && (Q + strip - 1) / strip <= 2 ? strip : 0;
 }
 
 template <typename T>

@@ -72,6 +72,14 @@ def test_backward(T, V, C, kind, dtype):
     _backward(_ids(kind, T, V), torch.randn(T, C, generator=g).to(DT[dtype]).cuda(), V, 2.5, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,C", [(210, 5, 65536), (1500, 3000, 1300), (2048, 9, 640), (2048, 9, 644), (2049, 70001, 36)])
+def test_backward_of_few_positions_and_many_channels(T, V, C, dtype):
+    """Both sides of the bound up to which no sort is done; few positions sorted, a large table cleared."""
+    g = torch.Generator().manual_seed(T)
+    _backward(_ids("padded", T, V), torch.randn(T, C, generator=g).to(DT[dtype]).cuda(), V, 0.5, dtype)
+
+
 @pytest.mark.parametrize("kind", ["empty", "sorted"])
 @pytest.mark.parametrize("T", [3, 300, 5000])
 def test_backward_without_symbols_and_in_order(kind, T):

@@ -191,6 +191,64 @@ def test_backward_over_many_tokens(shape, act):
         assert torch.equal(torch.isposinf(h["dW"][1]), want > 0) and torch.equal(torch.isneginf(h["dW"][1]), want < 0)
 
 
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("shape", [(2048, 64, 64), (4100, 64, 128), (4097, 128, 64), (8211, 64, 256), (8200, 256, 64),
+                                   (16411, 128, 256), (16400, 256, 128), (24577, 256, 512), (24603, 128, 384),
+                                   (49181, 256, 256)], ids=str)
+def test_backward_in_one_pass(shape, act):
+    """Every tile of the one-pass backward from the tokens at which it is taken."""
+    X, W, _, pre, d = _inputs(*shape, "bf16", seed=13)
+    pre = None if act == "none" else pre
+    g = fp.flarepp_linear_backward(X, W, d, pre=pre, act=ACTS[act])
+    _check_backward(X, W, pre, d, act, "bf16", g)
+    bad = X.clone()
+    bad[-1, 1] = float("inf")  # the last row, which a ragged step repeats
+    h = fp.flarepp_linear_backward(bad, W, d, pre=pre, act=ACTS[act])
+    keep = [k for k in range(shape[1]) if k != 1]
+    assert torch.equal(h["dX"], g["dX"]) and torch.equal(h["dbias"], g["dbias"]) and torch.equal(h["dW"][keep], g["dW"][keep])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(65536, 16, 40), (65539, 3, 64), (65540, 5, 256), (65537, 64, 4), (65600, 144, 32), (65541, 512, 31),
+                                   (65543, 32, 128), (65547, 30, 96), (65549, 16, 512), (98305, 128, 256), (98331, 256, 256),
+                                   (98304, 64, 512), (98307, 128, 288)], ids=str)
+def test_forward_over_the_rows(shape, dtype):
+    """The rows kernel from the rows at which it is taken: short rows, narrow
+    outputs, every strip width, two strips; also as the input gradient."""
+    T, K, N = shape
+    X, W, b, r, d = _inputs(T, K, N, dtype, seed=14)
+    out, pre = fp.flarepp_linear_forward(X, W, b, act=fp.ACT_SILU, residual=r, keep_pre=True)
+    dX = fp.flarepp_linear_backward(X, W, d, want_dW=False, want_dbias=False)["dX"]
+    for sl in (slice(0, 3000), slice(40000, 43000), slice(-3000, None)):  # rows are independent
+        _check_forward(X[sl], W, b, r[sl], "silu", dtype, out[sl], pre[sl])
+        _check_backward(X[sl], W, None, d[sl], "none", dtype, {"dX": dX[sl]})
+    buf = torch.full((T * N + 4096,), 7.0, dtype=X.dtype, device="cuda")  # what follows the last row stays
+    to = buf[:T * N].view(T, N)
+    fp.flarepp_linear_forward(X, W, b, act=fp.ACT_SILU, residual=r, out=to)
+    assert torch.equal(to, out) and (buf[T * N:] == 7).all()
+
+
+@pytest.mark.parametrize("shape", [(65600, 16, 64), (98400, 128, 256), (24600, 256, 512), (8000, 1000, 1000)], ids=str)
+def test_many_rows_captured(shape):
+    X, W, b, r, d = _inputs(*shape, "bf16", seed=15)
+    out, pre = fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, keep_pre=True)
+    g0 = fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_GELU)
+    o, gr = torch.empty_like(out), {k: torch.empty_like(v) for k, v in g0.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fp.flarepp_linear_forward(X, W, b, act=fp.ACT_GELU, out=o)
+        fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_GELU, out=gr)
+    for _ in range(3):
+        o.zero_()
+        for v in gr.values():
+            v.fill_(float("nan"))
+        fp.flarepp_linear_forward(r.new_ones(9, shape[1]), W)  # eager work in between
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, out) and all(torch.equal(gr[k], g0[k]) for k in g0)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(8192, 16, 32), (8195, 3, 64), (8200, 5, 256), (8193, 64, 4), (8200, 144, 33), (8192, 128, 256),
                                    (8300, 288, 128), (8192, 512, 256), (8192, 512, 512), (8201, 30, 96), (8195, 64, 160), (8192, 128, 288)], ids=str)
