@@ -140,8 +140,8 @@ LinPlan lin_plan(int prod, int bs, int64_t P, int64_t Q, int64_t K) {
   else { pl.tile = kTile64; bp = bq = 64; }
   if (pl.tile == kTile128 && !weight && bs == 2 && lin_direct(prod, bs, P, Q, K)) {
     // 256 x 256 where they fill the CUs' rounds to three quarters and pass the
-    // outputs' end by little: 8192 x 2048 -> 2048 66 / 71 us (128 x 128), 65,536 x 1024
-    // -> 512 76 / 93; 60,969 x 1248 -> 200 109 / 68, 50,000 x 640 -> 320 49 / 38
+    // outputs' end by little: with GELU 8192 x 2048 -> 2048 74 / 82 us (128 x 128), 65,536 x
+    // 1024 -> 512 91 / 106; but 60,969 x 1248 -> 200 99 / 72, 4096 x 2048 -> 2048 73 / 40
     const int64_t t = cdiv(P, 256) * cdiv(Q, 256);
     if (4 * t >= 3 * 256 * cdiv(t, 256) && 8 * cdiv(Q, 256) * 256 <= 9 * Q) { pl.tile = kTile256; bp = bq = 256; }
   }
