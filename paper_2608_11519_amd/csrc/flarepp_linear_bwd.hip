@@ -22,6 +22,9 @@ template <int NT> __device__ __forceinline__ int p_slot(int row, int s) {
 // sums dP in fp32, and with DX (K = KT, N = NT, the weights in LDS) dX = hi W^T
 // of the step is stored; else hi goes to memory for dX.  Beside a step's products
 // the next step's dP is formed, and the one after is loaded.
+// 131,072 x 128 -> 256, GELU: 62 us (and 8 for the sums over the chunks) for 201 MB, 39 us
+// at a large copy's rate; the VALU is busy for 36 us of it (some 40 instructions
+// per element of dP), the matrix cores for 10.
 template <int KT, int NT, bool SLOPE, bool DX> struct Bwd {
   static constexpr int KB = KT / 32, NB = NT / 32, BLOCKS = KB * NB;
   static constexpr int WB = BLOCKS >= 8 ? BLOCKS / 8 : 1;         // blocks of dW per wave, as BK x BN

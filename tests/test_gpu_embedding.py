@@ -138,3 +138,23 @@ def test_shapes_graph_and_stream():
         torch.cuda.synchronize()
         assert torch.equal(gr, want)
         assert torch.equal(o.view(torch.int16), fp.flarepp_embedding_forward(ids, table, scale=2.0).view(torch.int16))
+
+
+def test_offsets_past_32_bits():
+    """A table, a lookup and gradients of more than 2^32 elements."""
+    V, T, C = (1 << 22) + 9, (1 << 22) + 3, 1032
+    ids = torch.full((T,), -1, dtype=torch.int64, device="cuda")
+    ids[:2], ids[-3:] = torch.tensor([V - 1, 5], device="cuda"), torch.tensor([V - 2, V - 1, 0], device="cuda")
+    table = torch.zeros(V, C, dtype=torch.bfloat16, device="cuda")
+    table[-2:] = torch.randn(2, C, device="cuda").bfloat16()
+    table[5], table[0] = 3.0, -2.0
+    out = fp.flarepp_embedding_forward(ids, table, scale=2.0)
+    for t in (0, 1, 2, T // 2, T - 3, T - 2, T - 1):
+        want = table[ids[t]] * 2 if int(ids[t]) >= 0 else torch.zeros_like(table[0])
+        assert torch.equal(out[t], want)
+    out.zero_()
+    out[:2], out[-3:] = torch.randn(2, C, device="cuda").bfloat16(), torch.randn(3, C, device="cuda").bfloat16()
+    dT = fp.flarepp_embedding_backward(ids, out, V=V)
+    f = [out[i].float() for i in (0, 1, T - 3, T - 2, T - 1)]
+    assert torch.equal(dT[V - 1], f[0] + f[3]) and torch.equal(dT[5], f[1]) and torch.equal(dT[V - 2], f[2])
+    assert torch.equal(dT[0], f[4]) and not dT[6:V - 2].any() and not dT[1:5].any()

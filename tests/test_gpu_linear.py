@@ -349,3 +349,31 @@ def test_graph_replays_and_streams(shape):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(o, out) and all(torch.equal(gr[k], g0[k]) for k in g0)
+
+
+@pytest.mark.parametrize("shape", [(2100, 64, 64), (24600, 256, 512), (65536, 8, 300)], ids=str)
+def test_some_gradients_of_many_tokens(shape):
+    X, W, _, pre, d = _inputs(*shape, "bf16", seed=16)
+    for want in (("dX",), ("dW",), ("dbias",), ("dX", "dbias"), ("dW", "dbias"), ("dX", "dW")):
+        g = fp.flarepp_linear_backward(X, W, d, pre=pre, act=fp.ACT_GELU, **{f"want_{k}": k in want for k in ("dX", "dW", "dbias")})
+        assert set(g) == set(want)
+        _check_backward(X, W, pre, d, "gelu", "bf16", g)
+
+
+@pytest.mark.parametrize("shape", [(2 ** 25 + 37, 128, 64), (2 ** 26 + 5, 64, 3), (2 ** 24 + 33, 200, 260)], ids=str)
+def test_offsets_past_32_bits(shape):
+    """More than 2^32 elements or bytes of X: rows at the start and at the end, the others zero."""
+    T, K, N = shape
+    n = 300
+    x, W, b, _, dd = _inputs(2 * n, K, N, "bf16", seed=17)
+    X, d = torch.zeros(T, K, dtype=x.dtype, device="cuda"), torch.zeros(T, N, dtype=x.dtype, device="cuda")
+    for t, v in ((X, x), (d, dd)):
+        t[:n], t[-n:] = v[:n], v[n:]
+    out, pre = fp.flarepp_linear_forward(X, W, b, act=fp.ACT_RELU, keep_pre=True)
+    ends = lambda t: torch.cat([t[:n], t[-n:]])  # noqa: E731
+    _check_forward(x, W, b, None, "relu", "bf16", ends(out), ends(pre))
+    assert torch.equal(out[T // 2], torch.relu(b)) and torch.equal(out[T - n - 1], torch.relu(b))
+    # without activation zero rows of dOut add nothing, so the sums are those of the two ends
+    g = fp.flarepp_linear_backward(X, W, d)
+    g["dX"] = ends(g["dX"])
+    _check_backward(x, W, None, dd, "none", "bf16", g)
