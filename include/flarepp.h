@@ -1,6 +1,7 @@
 /*
  * flarepp.h -- C ABI of libflarepp.so, the FLARE++ mixer forward and
- * backward on AMD MI355X (gfx950).
+ * backward on AMD MI355X (gfx950), with the linear layer, the embedding and
+ * the optimiser step of a model around it.
  *
  * The operations follow "FLARE++: Low-rank attention with dynamic attention
  * routing" (arXiv 2608.11519):

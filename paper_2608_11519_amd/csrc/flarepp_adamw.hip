@@ -5,8 +5,8 @@
 // bounds it.  A wave takes blocks of 256 elements, whose 8-bit states share a
 // scale: one reduction over the wave.  The 8-bit states are m and sqrt(v), in e4m3,
 // rounded at random: a step moves sqrt(v) by far less than half a step of e4m3,
-// which rounding to the nearest would never pass.  8-bit states, 57.6 M elements:
-// 166 us, 5.4 TB/s (a large copy 5.2); three small tensors, fp32: 4.5 us.
+// which rounding to the nearest would never pass.  8-bit states, 49.6 M elements:
+// 166 us, 5.4 TB/s (a large copy 5.2); four small tensors, fp32: 4.5 us.
 #include <hip/hip_runtime.h>
 
 #include "flarepp_device.hpp"

@@ -178,9 +178,11 @@ size_t lin_rows_lds(int elem_bytes, int strip, int64_t K) {
 }
 
 // The strip for a product, or 0 where the tiles take less time.  Weights that
-// every CU copies pay over many rows only: from 65,536 where the inputs or the
-// outputs are few (rows / tiles, us: fp32 4 -> 64, 32,768 rows 7.7 / 7.2, 65,536 8.5 / 11.9;
-// bf16 64 -> 3, 24,576 4.5 / 4.5, 65,536 5.2 / 5.6), and in bf16 from 98,304 to outputs
+// every CU copies pay over many rows only: from 49,152 for at most 16 inputs
+// (rows / tiles, us: fp32 4 -> 64, 32,768 rows 7.7 / 7.2, 49,152 8.4 / 9.0; bf16 16 -> 256,
+// 24,576 16.5 / 12.2, 49,152 18.0 / 20.1), from 65,536 for at most 32 inputs or outputs
+// (bf16 64 -> 3, 24,576 4.5 / 4.5, 65,536 5.2 / 5.6; 32 -> 64, 49,152 7.0 / 6.6, 65,536 7.4 /
+// 8.9), and in bf16 from 98,304 to outputs
 // that are many and no fewer than the inputs, so that the stores are most of the
 // work (128 -> 256, 65,536 22 / 21, 100,000 35 / 37, 200,000 65 / 74; 256 -> 512, 65,536
 // 43 / 43, 200,000 133 / 150; not 256 -> 128, 200,000 48 / 47, nor fp32 256 -> 256, 257 / 257).
@@ -188,7 +190,7 @@ size_t lin_rows_lds(int elem_bytes, int strip, int64_t K) {
 // are whole blocks, or (forward) few; weights that fit, and L read at most twice.
 int lin_rows_strip(int prod, int elem_bytes, int64_t P, int64_t Q, int64_t K) {
   const bool whole = Q % 32 == 0, steps = K % 16 == 0, few = K <= 32 || Q <= 32;
-  if (few ? P < (1 << 16) : elem_bytes != 2 || P < (3 << 15) || Q < 256 || Q < K) return 0;
+  if (few ? P < (K <= 16 ? 3 << 14 : 1 << 16) : elem_bytes != 2 || P < (3 << 15) || Q < 256 || Q < K) return 0;
   if (prod == kLinWeight || K > 512 || (!steps && (K > 32 || !whole)) || (!whole && (prod != kLinForward || Q > 64))) return 0;
   const int widest = elem_bytes == 2 ? 256 : 64;
   int strip = 32;

@@ -210,7 +210,7 @@ def test_backward_in_one_pass(shape, act):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(65536, 16, 40), (65539, 3, 64), (65540, 5, 256), (65537, 64, 4), (65600, 144, 32), (65541, 512, 31),
-                                   (65543, 32, 128), (65547, 30, 96), (65549, 16, 512), (98305, 128, 256), (98331, 256, 256),
+                                   (65543, 32, 128), (65547, 30, 96), (65549, 16, 512), (49152, 3, 64), (49155, 16, 128), (98305, 128, 256), (98331, 256, 256),
                                    (98304, 64, 512), (98307, 128, 288)], ids=str)
 def test_forward_over_the_rows(shape, dtype):
     """The rows kernel from the rows at which it is taken: short rows, narrow
